@@ -222,13 +222,14 @@ def _loss(s):
     w = _weights(case, s["eff"])
     live = w > 0
     z = s["logits"].float() / t
-    z = z - z.amax(-1, keepdim=True)
+    top = z.amax(-1, keepdim=True)
+    z = z - top
     p = z.exp()
     total = p.sum(-1, keepdim=True, dtype=torch.float64)
     p = p / total.float()
     lp = z - total.log().float()                                  # log-probabilities
     ids = s["ids"].long()[..., None]
-    logp = z.gather(-1, ids)[..., 0].double() - total.log()[..., 0]
+    logp = (s["logits"].gather(-1, ids).double() / t - top.double() - total.log())[..., 0]
     plain = torch.where(p > 0, lp, 0.0)                           # 0 log 0 = 0
     entropy = -(p * plain).sum(-1, dtype=torch.float64)
     ratio = (logp - s["old"].double()).exp()
