@@ -272,6 +272,72 @@ int sol_reward_advantages(sol_ctx *ctx, const float *nll, const int32_t *action_
                           float *avg_out, float *penalty_out, float *returns_out, float *signal_out, float *adv_out,
                           void *workspace, size_t ws_bytes, void *stream);
 
+/* Policy update on the output of sol_reward_advantages (Method, "GRPO with per-sequence budget sampling": clipped policy updates with an
+ * entropy bonus). The three entry points below take every size from their arguments; the context gives the device (it must be the
+ * current one, else SOL_ERR_INVALID_ARG), the sticky flags and the error text. They run for any policy, whatever the context's model is.
+ *
+ * sol_policy_loss: loss of a categorical policy over A actions and its gradient by the logits. Row (b, g, t) of logits x, with
+ * logp_j = log softmax(x / temperature)_j, p_j = exp(logp_j), a = action_ids, d = logp_a - old_logp (old_logp NULL: 0, i.e. the
+ * policy that acted), rho = exp(d), w the row's share in the mean:
+ *   pg   = -min(rho adv, clip(rho, 1 - clip_low, 1 + clip_high) adv)
+ *   H    = -sum_j p_j logp_j                                        (0 log 0 = 0)
+ *   KL   = exp(u) - u - 1 with u = ref_logp - logp_a                (ref_logp given: the estimate from the action taken)
+ *        | sum_j p_j (logp_j - log softmax(ref_logits / temperature)_j)           (ref_logits given; neither: 0)
+ *   loss = scale * sum_rows w (pg + kl_coef KL - entropy_coef H)
+ * grad_out = d loss / d logits, old_logp, adv and the reference held fixed; the clipped branch of pg has no gradient.
+ * Rows of steps with eff[b][t] == 0 are not read: no part in the loss, gradient 0, logp 0. mean = SOL_MEAN_STEPS: w = 1 / (number of
+ * effective rows); SOL_MEAN_SCHEDULES: the effective steps of a schedule are averaged first, then the schedules that have any. Without
+ * any effective row the loss is 0. A logit of -inf forbids its action (p = 0, gradient 0); a row without an allowed action gives 0
+ * everywhere and logp -inf, and counts in the mean. NaN and +inf make the row, and the loss, NaN. An action id outside [0, A) counts
+ * as action 0 and sets the bad-action flag.
+ * logits: device [B][G][T] rows of A elements of dtype (sol_dtype), ld >= A elements apart; ref_logits likewise, ref_ld apart. adv (NULL:
+ * 0), old_logp, ref_logp: device float [B][G][T]; action_ids: device int32 [B][G][T]; eff: device int32 [B][T] or NULL (all). Outputs,
+ * device: loss_out float [1]; stats_out float [4], the means of pg, KL, H and of the share of clipped rows, or NULL; logp_out float
+ * [B][G][T], the actions' log-probabilities (the next update's old_logp), or NULL; grad_out rows of A elements of dtype, grad_ld
+ * apart, or NULL (loss alone). grad_out may be logits itself with grad_ld == ld; any other overlap with the logits is refused, and
+ * elements between the rows are left as they are. Sums are held in 32 bits per row and in 64 over the rows; a row's gradient is rounded
+ * once. Workspace: sol_policy_workspace_bytes(B, G, T). B * G * T == 0 is a no-op (loss_out is left as it is); at most 2^31 - 1 rows. */
+#define SOL_MEAN_STEPS 0
+#define SOL_MEAN_SCHEDULES 1
+typedef struct {
+    double  clip_low, clip_high;              /* the ratio's bounds are 1 - clip_low and 1 + clip_high; clip_low in [0, 1], clip_high >= 0 */
+    double  kl_coef, entropy_coef;            /* >= 0; kl_coef > 0 needs a reference */
+    double  temperature;                      /* > 0 */
+    double  scale;                            /* factor of loss and gradient (e.g. 1 / accumulated batches) */
+    int32_t mean;                             /* SOL_MEAN_STEPS or SOL_MEAN_SCHEDULES */
+} sol_policy_cfg;
+size_t sol_policy_workspace_bytes(int B, int G, int T);
+int sol_policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, const int32_t *action_ids, const float *adv,
+                    const float *old_logp, const float *ref_logp, const void *ref_logits, int64_t ref_ld, const int32_t *eff,
+                    const sol_policy_cfg *pc, int B, int G, int T, int A, float *loss_out, float *stats_out, float *logp_out,
+                    void *grad_out, int64_t grad_ld, void *workspace, size_t ws_bytes, void *stream);
+
+/* Global norm of many gradients, and clipping:
+ *   norm_out[0] = sqrt(sum over all elements of all tensors of g^2),  coef_out[0] = min(1, max_norm / (norm + eps)),
+ * and, with scale_grads != 0, every gradient is multiplied by coef in place (rounded to its type; untouched where coef is 1). The squares
+ * are summed in 64 bits. If the norm is not finite, coef_out is NaN and the gradients are left as they are. grads: HOST array of
+ * n_tensors entries (read during the call only, captured by value under graph capture): device data, elements, sol_dtype; contiguous,
+ * aligned to their elements, n == 0 allowed; overlapping ones are refused where they are scaled. max_norm > 0 (INFINITY: measure
+ * only). norm_out, coef_out: device float [1]. Workspace: sol_grad_clip_workspace_bytes(n_tensors). */
+typedef struct { void *data; int64_t n; int32_t dtype; int32_t reserved; } sol_grad;
+size_t sol_grad_clip_workspace_bytes(int n_tensors);
+int sol_grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double max_norm, double eps, int scale_grads, float *norm_out,
+                  float *coef_out, void *workspace, size_t ws_bytes, void *stream);
+
+/* AdamW over many tensors, t = step[0] the number of this update (from 1), g = coef[0] * grad (coef NULL: grad):
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *   param <- param (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   copy <- bf16(param)
+ * coef: device float [1], sol_grad_clip's coef_out, so that clipping costs no pass over the gradients: if it is NaN the call changes nothing.
+ * step: device int32 [1], advanced by the caller (also between replays of a captured call); below 1: nothing is changed and
+ * sol_device_status reports SOL_ERR_INVALID_ARG. lr: device float [1] in place of cfg.lr, or NULL. tensors: HOST array as in
+ * sol_grad_clip; param, m, v: device float [n]; grad: device [n] of grad_dtype, read only; copy: device bf16 [n] or NULL, what a bf16
+ * forward pass reads (parameters and moments stay in 32 bits: a bf16 parameter would lose updates below 2^-9 of its value). Tensors that
+ * are written must not overlap each other or a gradient (refused). No workspace. */
+typedef struct { float *param, *m, *v; const void *grad; void *copy; int64_t n; int32_t grad_dtype; int32_t reserved; } sol_adamw_tensor;
+typedef struct { double lr, beta1, beta2, eps, weight_decay; } sol_adamw_cfg;   /* betas in [0, 1), the others >= 0 */
+int sol_adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tensors, const sol_adamw_cfg *ac, const int32_t *step,
+                   const float *lr, const float *coef, void *stream);
+
 /* Teacher-forced pass over G compute schedules that share one token path (Method, "GRPO with
  * per-sequence budget sampling"): for every input b, schedule g and position t,
  *   nll_out[b][g][t] = -log p_t^{a}(targets[b][t])  in nats (Method, Eq. 1, negated),
@@ -285,9 +351,10 @@ int sol_schedule_loglik(sol_ctx *ctx, const sol_model_weights *weights,
 
 /* Synchronises `stream`, returns and clears the sticky device flags:
  * SOL_OK, SOL_ERR_CACHE_OVERFLOW (a sequence was skipped because pos0 + T > L_max), SOL_ERR_ACTION (an action id
- * outside the table was met and treated as dense) or SOL_ERR_INVALID_ARG (a token id or a target id outside
- * [0, vocab) was met and clamped into it: the embedding lookups and the NLLs of sol_schedule_loglik,
- * sol_episode_loglik, sol_decode_step and sol_kv_refresh of that call are then those of the clamped ids). */
+ * outside the table was met and treated as dense, by sol_reward_advantages and sol_policy_loss as action 0) or
+ * SOL_ERR_INVALID_ARG (a token id or a target id outside [0, vocab) was met and clamped into it: the embedding lookups and the
+ * NLLs of sol_schedule_loglik, sol_episode_loglik, sol_decode_step and sol_kv_refresh of that call are then those of the
+ * clamped ids; or an update's step was below 1, see sol_adamw_step). */
 int sol_device_status(sol_ctx *ctx, void *stream);
 
 /* Per-stage timing for measurement. sol_profile_enable(ctx, n) with n > 0 creates up to n pairs of

@@ -353,3 +353,81 @@ def reward_advantages(nll, action_ids, actions, targets, alpha, tau, gamma, eff=
     centred = signal - signal.mean(axis=1, keepdims=True)
     adv = (centred - centred.mean()) / (centred.std() + eps)
     return {"avg": avg, "penalty": pen, "returns": ret, "signal": signal, "adv": adv}
+
+
+# ---------------------------------------------------------------------------------------------------
+# policy update (Method, "GRPO with per-sequence budget sampling": clipped policy updates with an entropy bonus): plain numpy in
+# float64, row by row
+# ---------------------------------------------------------------------------------------------------
+def _log_softmax(x, temperature):
+    z = np.asarray(x, np.float64) / temperature
+    with np.errstate(invalid="ignore", divide="ignore"):
+        m = z.max()
+        return z - m - np.log(np.exp(z - m).sum())
+
+
+def policy_loss(logits, action_ids, adv=None, old_logp=None, ref_logp=None, ref_logits=None, eff=None, clip=(0.2, 0.2), kl_coef=0.0,
+                entropy_coef=0.0, temperature=1.0, scale=1.0, mean="steps"):
+    """logits [B][G][T][A]; the definitions of include/sol.h, a row at a time. Returns dict: loss, stats [4] (policy term, KL, entropy,
+    clipped share), logp [B][G][T], grad [B][G][T][A], size [B][G][T][A]: the sum of the magnitudes that a gradient is the sum of (what its
+    rounding errors are relative to), ratio [B][G][T]."""
+    x = np.asarray(logits, np.float64)
+    B, G, T, A = x.shape
+    e = np.ones((B, T), bool) if eff is None else np.asarray(eff) != 0
+    n = e.sum(1)
+    out = {"logp": np.zeros((B, G, T)), "grad": np.zeros(x.shape), "size": np.zeros(x.shape), "ratio": np.ones((B, G, T))}
+    stats = np.zeros(4)
+    for b, g, t in np.ndindex(B, G, T):
+        if not e[b, t]:
+            continue
+        w = 1.0 / (G * n.sum()) if mean == "steps" else 1.0 / (n[b] * G * (n > 0).sum())
+        if np.all(x[b, g, t] == -np.inf):
+            out["logp"][b, g, t] = -np.inf
+            continue
+        lp = _log_softmax(x[b, g, t], temperature)
+        a = action_ids[b, g, t] if 0 <= action_ids[b, g, t] < A else 0
+        p = np.exp(lp)
+        some = p > 0
+        lp0 = np.where(some, lp, 0.0)
+        logp, advantage = lp[a], 0.0 if adv is None else float(adv[b, g, t])
+        ratio = 1.0 if old_logp is None else np.exp(logp - float(old_logp[b, g, t]))
+        free, held = ratio * advantage, np.clip(ratio, 1 - clip[0], 1 + clip[1]) * advantage
+        clipped = held < free
+        by_logp, kl, far = 0.0 if clipped else -free, 0.0, np.zeros(A)
+        entropy = -(p * lp0).sum()
+        if ref_logp is not None:
+            u = float(ref_logp[b, g, t]) - logp
+            kl = np.expm1(u) - u
+            by_logp -= kl_coef * np.expm1(u)
+        if ref_logits is not None:
+            far = np.where(some, lp0 - np.where(some, _log_softmax(ref_logits[b, g, t], temperature), 0.0), 0.0)
+            kl = (p * far).sum()
+        hot = np.zeros(A)
+        hot[a] = 1.0
+        f = w * scale / temperature
+        exact = 0.0 if ref_logits is None else kl_coef
+        out["grad"][b, g, t] = f * (by_logp * (hot - p) + exact * p * (far - kl) + entropy_coef * p * (lp0 + entropy))
+        out["size"][b, g, t] = f * (abs(by_logp) * (hot + p) + exact * p * (abs(far) + abs(kl)) + entropy_coef * p * (abs(lp0) + entropy))
+        out["logp"][b, g, t], out["ratio"][b, g, t] = logp, ratio
+        stats += w * np.array([-min(free, held), kl, entropy, float(clipped)])
+    out["stats"] = stats
+    out["loss"] = scale * (stats[0] + kl_coef * stats[1] - entropy_coef * stats[2])
+    return out
+
+
+def grad_clip(grads, max_norm, eps=1e-6):
+    """(norm, coefficient, scaled gradients) of a list of arrays."""
+    grads = [np.asarray(g, np.float64) for g in grads]
+    norm = float(np.sqrt(sum((g * g).sum() for g in grads)))
+    coef = min(1.0, max_norm / (norm + eps))
+    return norm, coef, [g * coef for g in grads]
+
+
+def adamw_step(p, g, m, v, t, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, coef=1.0):
+    """One tensor's (param, m, v) after update t."""
+    p, g, m, v = (np.asarray(a, np.float64) for a in (p, g, m, v))
+    g = coef * g
+    m = betas[0] * m + (1 - betas[0]) * g
+    v = betas[1] * v + (1 - betas[1]) * g * g
+    p = p * (1 - lr * weight_decay) - lr * (m / (1 - betas[0] ** t)) / (np.sqrt(v / (1 - betas[1] ** t)) + eps)
+    return p, m, v

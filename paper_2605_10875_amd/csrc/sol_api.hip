@@ -2,6 +2,7 @@
 // action-conditioned decoder layer, the decode step and the teacher-forced schedule pass.
 #include "../../include/sol.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -234,8 +235,9 @@ extern "C" int sol_device_status(sol_ctx *ctx, void *stream)
     SOL_HIP(ctx, hipMemcpy(&f, ctx->d_flags, sizeof(int), hipMemcpyDeviceToHost));
     if (f) SOL_HIP(ctx, hipMemset(ctx->d_flags, 0, sizeof(int)));
     if (f & FLAG_CACHE_OVERFLOW) return fail(ctx, SOL_ERR_CACHE_OVERFLOW, "a sequence's tokens did not fit its cache and were skipped");
-    if (f & FLAG_BAD_ACTION) return fail(ctx, SOL_ERR_ACTION, "an action id outside the table was treated as the dense action");
+    if (f & FLAG_BAD_ACTION) return fail(ctx, SOL_ERR_ACTION, "an action id outside the table was treated as the dense action (in a reduction or a policy loss: as action 0)");
     if (f & FLAG_BAD_TOKEN) return fail(ctx, SOL_ERR_INVALID_ARG, "a token or target id outside the vocabulary was clamped into it");
+    if (f & FLAG_BAD_STEP) return fail(ctx, SOL_ERR_INVALID_ARG, "an update's step was below 1: nothing was updated");
     return SOL_OK;
 }
 
@@ -927,6 +929,184 @@ extern "C" int sol_reward_advantages(sol_ctx *ctx, const float *nll, const int32
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(ctx, SOL_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
     return SOL_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// policy update: loss and gradient over the actions, gradient norm and clip, AdamW
+// ------------------------------------------------------------------------------------------------
+// These entry points take sizes and pointers from their arguments alone; the context gives the device, the flags and the error text.
+static int on_device(sol_ctx *ctx)
+{
+    int device = -1;
+    SOL_HIP(ctx, hipGetDevice(&device));
+    if (device != ctx->device) return fail(ctx, SOL_ERR_INVALID_ARG, "the current device is not the context's");
+    return SOL_OK;
+}
+
+static int launched(sol_ctx *ctx)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SOL_OK : fail(ctx, SOL_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
+}
+
+struct Range { uintptr_t from, to; };                          // bytes [from, to)
+static Range range_of(const void *p, uint64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + bytes}; }
+static bool meet(const Range &a, const Range &b) { return a.from < b.to && b.from < a.to; }
+// whether any two of them meet (sorts them)
+static bool any_meet(std::vector<Range> &r)
+{
+    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
+    for (size_t i = 1; i < r.size(); ++i) if (r[i].from < r[i - 1].to) return true;
+    return false;
+}
+
+extern "C" size_t sol_policy_workspace_bytes(int B, int G, int T)
+{
+    if (B <= 0 || G <= 0 || T <= 0) return 0;
+    return policy_scratch_bytes(B) + 256;
+}
+
+static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, const int32_t *action_ids, const float *adv,
+                       const float *old_logp, const float *ref_logp, const void *ref_logits, int64_t ref_ld, const int32_t *eff,
+                       const sol_policy_cfg *pc, int B, int G, int T, int A, float *loss_out, float *stats_out, float *logp_out,
+                       void *grad_out, int64_t grad_ld, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (B < 0 || G < 0 || T < 0 || A <= 0) return fail(ctx, SOL_ERR_INVALID_ARG, "negative size, or no action");
+    if (!pc || !loss_out) return fail(ctx, SOL_ERR_INVALID_ARG, "cfg or loss_out is NULL");
+    auto weight = [](double v) { return v >= 0.0 && v < INFINITY; };
+    if (!(pc->clip_low >= 0.0 && pc->clip_low <= 1.0) || !(pc->clip_high >= 0.0) || !weight(pc->kl_coef) || !weight(pc->entropy_coef) ||
+        !(pc->temperature > 0.0 && pc->temperature < INFINITY) || !std::isfinite(pc->scale))
+        return fail(ctx, SOL_ERR_INVALID_ARG, "policy cfg: clip_low in [0, 1], clip_high >= 0, coefficients >= 0 and finite, temperature > 0, scale finite");
+    if (pc->mean != SOL_MEAN_STEPS && pc->mean != SOL_MEAN_SCHEDULES) return fail(ctx, SOL_ERR_INVALID_ARG, "policy cfg: unknown mean");
+    if (dtype != SOL_F32 && dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, "dtype must be SOL_F32 or SOL_BF16");
+    if (ref_logp && ref_logits) return fail(ctx, SOL_ERR_INVALID_ARG, "ref_logp and ref_logits exclude each other");
+    if (pc->kl_coef > 0.0 && !ref_logp && !ref_logits) return fail(ctx, SOL_ERR_INVALID_ARG, "kl_coef > 0 without a reference");
+    if (ld < A || (ref_logits && ref_ld < A) || (grad_out && grad_ld < A)) return fail(ctx, SOL_ERR_INVALID_ARG, "rows closer than their length");
+    const bool none = B == 0 || G == 0 || T == 0;
+    if (!none && (int64_t)B * G > INT32_MAX / T) return fail(ctx, SOL_ERR_UNSUPPORTED, "2^31 rows or more");
+    const int64_t rows = none ? 0 : (int64_t)B * G * T;
+    if (none) return SOL_OK;                                    // a mean over nothing: the loss stays as it was
+    if (!logits || !action_ids) return fail(ctx, SOL_ERR_INVALID_ARG, "a data pointer is NULL");
+    const size_t es = esize(dtype);
+    if ((uintptr_t)logits % es || (uintptr_t)ref_logits % es || (uintptr_t)grad_out % es) return fail(ctx, SOL_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+    auto span = [&](const void *p, int64_t step) { return range_of(p, ((uint64_t)(rows - 1) * (uint64_t)step + (uint64_t)A) * es); };
+    if (grad_out) {                                             // in place row by row, or apart
+        const Range g = span(grad_out, grad_ld);
+        if (!(grad_out == logits && grad_ld == ld) && meet(g, span(logits, ld))) return fail(ctx, SOL_ERR_INVALID_ARG, "grad_out overlaps logits");
+        if (ref_logits && meet(g, span(ref_logits, ref_ld))) return fail(ctx, SOL_ERR_INVALID_ARG, "grad_out overlaps ref_logits");
+    }
+    if (logp_out && (logp_out == adv || logp_out == old_logp || logp_out == ref_logp)) return fail(ctx, SOL_ERR_INVALID_ARG, "logp_out must not alias an input");
+    const size_t need = sol_policy_workspace_bytes(B, G, T);
+    if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
+    if (const int rc = on_device(ctx)) return rc;
+    Carver c(workspace);
+    PolicyArgs q{};
+    q.logits = logits; q.ref_logits = ref_logits; q.grad = grad_out;
+    q.ld = ld; q.ref_ld = ref_ld; q.grad_ld = grad_ld;
+    q.ids = action_ids; q.eff = eff; q.adv = adv; q.old_logp = old_logp; q.ref_logp = ref_logp;
+    q.loss = loss_out; q.stats = stats_out; q.logp = logp_out; q.flags = ctx->d_flags;
+    q.dtype = dtype; q.B = B; q.G = G; q.T = T; q.A = A;
+    launch_policy_loss(q, PolicyCfg{pc->clip_low, pc->clip_high, pc->kl_coef, pc->entropy_coef, pc->temperature, pc->scale, pc->mean == SOL_MEAN_SCHEDULES},
+                       c.take(policy_scratch_bytes(B)), (hipStream_t)stream);
+    return launched(ctx);
+}
+
+extern "C" int sol_policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, const int32_t *action_ids, const float *adv,
+                               const float *old_logp, const float *ref_logp, const void *ref_logits, int64_t ref_ld,
+                               const int32_t *eff, const sol_policy_cfg *pc, int B, int G, int T, int A, float *loss_out,
+                               float *stats_out, float *logp_out, void *grad_out, int64_t grad_ld, void *workspace,
+                               size_t ws_bytes, void *stream)
+{
+    if (!ctx) return SOL_ERR_INVALID_ARG;
+    try {
+        return policy_loss(ctx, logits, dtype, ld, action_ids, adv, old_logp, ref_logp, ref_logits, ref_ld, eff, pc, B, G, T, A, loss_out,
+                           stats_out, logp_out, grad_out, grad_ld, workspace, ws_bytes, stream);
+    } catch (...) { return SOL_ERR_HIP; }                       // (no memory on the host)
+}
+
+extern "C" size_t sol_grad_clip_workspace_bytes(int n_tensors) { return n_tensors < 0 ? 0 : clip_scratch_bytes(n_tensors) + 256; }
+
+static int grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double max_norm, double eps, int scale_grads, float *norm_out,
+                     float *coef_out, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (n_tensors < 0 || (n_tensors > 0 && !grads)) return fail(ctx, SOL_ERR_INVALID_ARG, "no list of gradients");
+    if (!norm_out || !coef_out) return fail(ctx, SOL_ERR_INVALID_ARG, "norm_out or coef_out is NULL");
+    if (!(max_norm > 0.0) || !(eps >= 0.0 && eps < INFINITY)) return fail(ctx, SOL_ERR_INVALID_ARG, "max_norm must be > 0, eps >= 0 and finite");
+    std::vector<GradItem> items((size_t)n_tensors);
+    std::vector<Range> at;
+    at.reserve((size_t)n_tensors);
+    for (int i = 0; i < n_tensors; ++i) {
+        const sol_grad &g = grads[i];
+        const std::string which = "gradient " + std::to_string(i);
+        if (g.n < 0 || (g.n > 0 && !g.data)) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": no data");
+        if (g.dtype != SOL_F32 && g.dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": dtype must be SOL_F32 or SOL_BF16");
+        if ((uintptr_t)g.data % esize(g.dtype)) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": not aligned to its elements");
+        items[i] = GradItem{g.data, g.n, g.dtype};
+        if (g.n) at.push_back(range_of(g.data, (uint64_t)g.n * esize(g.dtype)));
+    }
+    if (scale_grads && any_meet(at)) return fail(ctx, SOL_ERR_INVALID_ARG, "two gradients overlap");
+    const size_t need = sol_grad_clip_workspace_bytes(n_tensors);
+    if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
+    if (const int rc = on_device(ctx)) return rc;
+    Carver c(workspace);
+    launch_grad_clip(items.data(), n_tensors, max_norm, eps, scale_grads != 0, norm_out, coef_out, c.take(clip_scratch_bytes(n_tensors)),
+                     (hipStream_t)stream);
+    return launched(ctx);
+}
+
+extern "C" int sol_grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double max_norm, double eps, int scale_grads,
+                             float *norm_out, float *coef_out, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (!ctx) return SOL_ERR_INVALID_ARG;
+    try {
+        return grad_clip(ctx, grads, n_tensors, max_norm, eps, scale_grads, norm_out, coef_out, workspace, ws_bytes, stream);
+    } catch (...) { return SOL_ERR_HIP; }
+}
+
+static int adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tensors, const sol_adamw_cfg *ac, const int32_t *step,
+                      const float *lr, const float *coef, void *stream)
+{
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return fail(ctx, SOL_ERR_INVALID_ARG, "no list of tensors");
+    if (!ac || !step) return fail(ctx, SOL_ERR_INVALID_ARG, "cfg or step is NULL");
+    auto rate = [](double b) { return b >= 0.0 && b < 1.0; };
+    if (!(ac->lr >= 0.0 && ac->lr < INFINITY) || !rate(ac->beta1) || !rate(ac->beta2) || !(ac->eps >= 0.0 && ac->eps < INFINITY) ||
+        !(ac->weight_decay >= 0.0 && ac->weight_decay < INFINITY))
+        return fail(ctx, SOL_ERR_INVALID_ARG, "adamw cfg: lr, eps, weight_decay must be >= 0 and finite, the betas in [0, 1)");
+    std::vector<AdamItem> items((size_t)n_tensors);
+    std::vector<Range> at, read;
+    at.reserve(4 * (size_t)n_tensors);
+    read.reserve((size_t)n_tensors);
+    for (int i = 0; i < n_tensors; ++i) {
+        const sol_adamw_tensor &t = tensors[i];
+        const std::string which = "tensor " + std::to_string(i);
+        if (t.n < 0 || (t.n > 0 && (!t.param || !t.m || !t.v || !t.grad))) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": no data");
+        if (t.grad_dtype != SOL_F32 && t.grad_dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": grad_dtype must be SOL_F32 or SOL_BF16");
+        if (((uintptr_t)t.param | (uintptr_t)t.m | (uintptr_t)t.v) % 4 || (uintptr_t)t.grad % esize(t.grad_dtype) || (uintptr_t)t.copy % 2)
+            return fail(ctx, SOL_ERR_INVALID_ARG, which + ": not aligned to its elements");
+        items[i] = AdamItem{t.param, t.m, t.v, t.grad, t.copy, t.n, t.grad_dtype};
+        if (!t.n) continue;
+        for (const float *p : {t.param, t.m, t.v}) at.push_back(range_of(p, 4 * (uint64_t)t.n));
+        if (t.copy) at.push_back(range_of(t.copy, 2 * (uint64_t)t.n));
+        read.push_back(range_of(t.grad, (uint64_t)t.n * esize(t.grad_dtype)));
+    }
+    if (any_meet(at)) return fail(ctx, SOL_ERR_INVALID_ARG, "two of the tensors to be written overlap");
+    for (const Range &g : read) {                               // a gradient may serve two tensors, but nothing is written into it
+        const auto after = std::lower_bound(at.begin(), at.end(), g.to, [](const Range &r, uintptr_t v) { return r.from < v; });
+        if (after != at.begin() && meet(*(after - 1), g)) return fail(ctx, SOL_ERR_INVALID_ARG, "a gradient overlaps a tensor to be written");
+    }
+    if (const int rc = on_device(ctx)) return rc;
+    launch_adamw(items.data(), n_tensors, AdamCfg{ac->lr, ac->beta1, ac->beta2, ac->eps, ac->weight_decay}, step, lr, coef, ctx->d_flags,
+                 (hipStream_t)stream);
+    return launched(ctx);
+}
+
+extern "C" int sol_adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tensors, const sol_adamw_cfg *ac,
+                              const int32_t *step, const float *lr, const float *coef, void *stream)
+{
+    if (!ctx) return SOL_ERR_INVALID_ARG;
+    try {
+        return adamw_step(ctx, tensors, n_tensors, ac, step, lr, coef, stream);
+    } catch (...) { return SOL_ERR_HIP; }
 }
 
 // ------------------------------------------------------------------------------------------------

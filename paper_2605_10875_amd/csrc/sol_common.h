@@ -18,7 +18,7 @@ struct RowAct {
     int32_t  bits;                // activation bit-width; >= 16 bypasses the quantiser
 };
 
-enum { FLAG_BAD_ACTION = 1, FLAG_CACHE_OVERFLOW = 2, FLAG_BAD_TOKEN = 4 };
+enum { FLAG_BAD_ACTION = 1, FLAG_CACHE_OVERFLOW = 2, FLAG_BAD_TOKEN = 4, FLAG_BAD_STEP = 8 };
 
 // f(0), .., f(N - 1), the arguments integral constants
 template <int... I, class F> __device__ __forceinline__ void static_for_(std::integer_sequence<int, I...>, F &&f)

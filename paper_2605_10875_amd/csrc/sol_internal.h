@@ -238,4 +238,29 @@ void launch_reward(const float *nll, const int32_t *ids, const ActionDev *table,
                    float *ret_out, float *signal, float *adv, void *scratch, int *flags, hipStream_t st);
 size_t reward_scratch_bytes(int B, int T);
 
+// ---- clipped policy loss (sol_policy.hip) -------------------------------------------------------
+struct PolicyArgs {
+    const void *logits, *ref_logits;          // rows of A elements of dtype, ld / ref_ld elements apart; ref_logits may be NULL
+    void *grad;                               // rows grad_ld apart, NULL or the logits' own rows among others
+    int64_t ld, ref_ld, grad_ld;
+    const int32_t *ids, *eff;                 // [rows]; [B][T] or NULL
+    const float *adv, *old_logp, *ref_logp;   // [rows], each may be NULL
+    float *loss, *stats, *logp;               // [1], [4] or NULL, [rows] or NULL
+    int *flags;
+    int dtype, B, G, T, A;                    // rows = B * G * T < 2^31
+};
+struct PolicyCfg { double clip_low, clip_high, kl_coef, entropy_coef, temperature, scale; int by_schedule; };
+size_t policy_scratch_bytes(int B);
+void launch_policy_loss(const PolicyArgs &q, const PolicyCfg &g, void *scratch, hipStream_t st);
+
+// ---- gradient norm, clip and AdamW over many tensors (sol_update.hip) ----------------------------
+struct GradItem { void *g; int64_t n; int dtype; };
+struct AdamItem { float *p, *m, *v; const void *g; void *copy; int64_t n; int dtype; };
+struct AdamCfg { double lr, beta1, beta2, eps, weight_decay; };
+size_t clip_scratch_bytes(int count);
+void launch_grad_clip(const GradItem *items, int count, double max_norm, double eps, bool scale, float *norm, float *coef, void *scratch,
+                      hipStream_t st);
+void launch_adamw(const AdamItem *items, int count, const AdamCfg &a, const int32_t *step, const float *lr_dev, const float *coef,
+                  int *flags, hipStream_t st);
+
 }  // namespace sol

@@ -24,6 +24,7 @@ EXPORTS = ("sol_validate_config", "sol_create", "sol_destroy", "sol_last_error",
            "sol_layer_forward", "sol_decode_step", "sol_schedule_loglik", "sol_device_status",
            "sol_page_meta_bytes", "sol_page_meta_build", "sol_decode_step_paged", "sol_kv_refresh",
            "sol_reward_advantages", "sol_episode_workspace_bytes", "sol_episode_loglik",
+           "sol_policy_workspace_bytes", "sol_policy_loss", "sol_grad_clip_workspace_bytes", "sol_grad_clip", "sol_adamw_step",
            "sol_profile_enable", "sol_profile_read",
            "sol_test_topk_select", "sol_test_prune_mask", "sol_test_prune_quant", "sol_test_quant_codes",
            "sol_test_gemm", "sol_test_attn_threshold", "sol_test_attention_stage", "sol_test_mlp_stage",
@@ -34,6 +35,15 @@ EXPORTS = ("sol_validate_config", "sol_create", "sol_destroy", "sol_last_error",
 class RewardCfg(C.Structure):
     _fields_ = [("alpha_kappa", C.c_float), ("alpha_rho", C.c_float), ("alpha_eta", C.c_float), ("tau", C.c_float),
                 ("gamma", C.c_float), ("eps", C.c_float)]
+
+
+class PolicyCfg(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double), ("entropy_coef", C.c_double),
+                ("temperature", C.c_double), ("scale", C.c_double), ("mean", C.c_int32)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double)]
 
 
 class ActionDef(C.Structure):
@@ -116,6 +126,17 @@ def lib():
         L.sol_reward_advantages.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                             C.POINTER(RewardCfg), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sol_policy_workspace_bytes.restype = C.c_size_t
+        L.sol_policy_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+        L.sol_policy_loss.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(PolicyCfg), C.c_int, C.c_int, C.c_int, C.c_int,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sol_grad_clip_workspace_bytes.restype = C.c_size_t
+        L.sol_grad_clip_workspace_bytes.argtypes = [C.c_int]
+        L.sol_grad_clip.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_double, C.c_double, C.c_int, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sol_adamw_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.POINTER(AdamwCfg), C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p]
         L.sol_episode_workspace_bytes.restype = C.c_size_t
         L.sol_episode_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int, C.c_int, C.c_int]
         L.sol_episode_loglik.argtypes = [C.c_void_p, C.POINTER(ModelWeights), C.c_void_p, C.c_void_p, C.c_void_p,
@@ -201,6 +222,58 @@ def _dtype_code(t):
 def _i32(t):
     assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous())
     return t
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(t, dtype, shape, what):
+    """A contiguous tensor of the current device, or None."""
+    if t is not None:
+        _need(t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape),
+              f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the GPU is needed")
+        _need(t.device.index == torch.cuda.current_device(), f"{what}: not on the current device")
+    return t
+
+
+def _row_step(t, what):
+    """Elements from one row of t ([..][A], rows evenly spaced) to the next."""
+    A = t.shape[-1]
+    if t.is_contiguous():
+        return A
+    _need(A == 1 or t.stride(-1) == 1, f"{what}: the elements of a row have to be adjacent")
+    step, rows = 0, 1
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size != 1:
+            step = step or stride
+            _need(rows == 1 or stride == step * rows, f"{what}: the rows have to be evenly spaced")
+            rows *= size
+    step = step or A
+    _need(step >= A, f"{what}: the rows overlap")
+    return step
+
+
+def _flat(ts, dtypes, what):
+    """The tensors of a list: contiguous, of one of these types, on the current device."""
+    here = torch.cuda.current_device()
+    for i, t in enumerate(ts):
+        if t.dtype not in dtypes or t.get_device() != here or not t.is_contiguous():
+            raise ValueError(f"{what}[{i}]: a contiguous tensor of {' or '.join(map(str, dtypes))} on the current device is needed")
+    return ts
+
+
+def _used_on(stream, *ts):
+    """Tensors made here that another stream works on: their memory is not given away before it is done."""
+    if stream is not None:
+        for t in ts:
+            if t is not None:
+                t.record_stream(stream)
+
+
+_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+MEANS = {"steps": 0, "schedules": 1}
 
 
 class Sol:
@@ -419,6 +492,84 @@ class Sol:
                                                  _ptr(out["penalty"]), _ptr(out["returns"]), _ptr(out["signal"]),
                                                  _ptr(out["adv"]), _ptr(ws), ws.numel(), _stream(stream)))
         return out
+
+    def policy_loss(self, logits, action_ids, adv=None, old_logp=None, ref_logp=None, ref_logits=None, eff=None, clip=(0.2, 0.2),
+                    kl_coef=0.0, entropy_coef=0.0, temperature=1.0, scale=1.0, mean="steps", want_grad=True, grad_out=None,
+                    stream=None):
+        """Clipped policy loss with KL term and entropy bonus of logits [B][G][T][A] (float32 or bfloat16, rows evenly spaced),
+        forward and gradient. action_ids int32, adv / old_logp / ref_logp float32 [B][G][T] or None, ref_logits like logits or
+        None, eff int32 [B][T] or None. Returns dict of device tensors: loss [1], stats [4] (policy term, KL, entropy, clipped
+        share), logp [B][G][T], grad like logits (grad_out if given, which may be logits itself; None if want_grad is false)."""
+        _need(logits.dim() == 4 and logits.dtype in _CODE, "logits: [B][G][T][A] of float32 or bfloat16 is needed")
+        _need(logits.is_cuda and logits.device.index == torch.cuda.current_device(), "logits: not on the current device")
+        _need(mean in MEANS, f"mean: one of {', '.join(MEANS)}")
+        B, G, T, A = logits.shape
+        ld = _row_step(logits, "logits")
+        steps = (B, G, T)
+        for t, what in ((adv, "adv"), (old_logp, "old_logp"), (ref_logp, "ref_logp")):
+            _on(t, torch.float32, steps, what)
+        _need(action_ids is not None, "action_ids are needed")
+        _on(action_ids, torch.int32, steps, "action_ids")
+        _on(eff, torch.int32, (B, T), "eff")
+        for t, what in ((ref_logits, "ref_logits"), (grad_out, "grad_out")):
+            if t is not None:
+                _need(t.shape == logits.shape and t.dtype == logits.dtype and t.device == logits.device, f"{what}: not like logits")
+        if want_grad and grad_out is None:
+            grad_out = torch.empty((B, G, T, A), dtype=logits.dtype, device=logits.device)
+        loss = torch.zeros(1, dtype=torch.float32, device=logits.device) if B * G * T == 0 else logits.new_empty(1, dtype=torch.float32)
+        stats, logp = loss.new_zeros(4) if B * G * T == 0 else loss.new_empty(4), loss.new_empty(steps)
+        ws = loss.new_empty(self.L.sol_policy_workspace_bytes(B, G, T), dtype=torch.uint8)
+        cfg = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean])
+        grad = grad_out if want_grad else None
+        self._check(self.L.sol_policy_loss(
+            self.handle, _ptr(logits), _CODE[logits.dtype], ld, _ptr(action_ids), _ptr(adv), _ptr(old_logp), _ptr(ref_logp),
+            _ptr(ref_logits), _row_step(ref_logits, "ref_logits") if ref_logits is not None else 0, _ptr(eff), C.byref(cfg), B, G, T, A,
+            _ptr(loss), _ptr(stats), _ptr(logp), _ptr(grad), _row_step(grad, "grad_out") if grad is not None else 0, _ptr(ws),
+            ws.numel(), _stream(stream)))
+        _used_on(stream, ws, loss, stats, logp, grad)
+        return {"loss": loss, "stats": stats, "logp": logp, "grad": grad}
+
+    def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
+        """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
+        [1] on the device; scale: the gradients are multiplied by coef in place. Nothing is synchronised."""
+        _flat(grads, _CODE, "grads")
+        arr = (C.c_int64 * (3 * len(grads)))(*[v for g in grads for v in (g.data_ptr(), g.numel(), _CODE[g.dtype])])
+        out = torch.empty(2, dtype=torch.float32, device="cuda")
+        ws = torch.empty(self.L.sol_grad_clip_workspace_bytes(len(grads)), dtype=torch.uint8, device="cuda")
+        norm, coef = out[:1], out[1:]
+        self._check(self.L.sol_grad_clip(self.handle, arr, len(grads), max_norm, eps, int(bool(scale)), _ptr(norm), _ptr(coef), _ptr(ws),
+                                         ws.numel(), _stream(stream)))
+        _used_on(stream, ws, out)
+        return norm, coef
+
+    def adamw_step(self, params, grads, exp_avg, exp_avg_sq, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, coef=None,
+                   copies=None, stream=None):
+        """AdamW on lists of contiguous tensors: params, exp_avg, exp_avg_sq float32, grads float32 or bfloat16, copies bfloat16
+        (rounded parameters for the forward pass) or None. step: int32 [1] on the device, the number of this update from 1; lr: a
+        number, or float32 [1] on the device; coef: grad_clip's coefficient, by which the gradients are multiplied on the way, or None."""
+        n = len(params)
+        _need(len(grads) == n and len(exp_avg) == n and len(exp_avg_sq) == n and (copies is None or len(copies) == n),
+              "the lists differ in length")
+        f32 = (torch.float32,)
+        _flat(params, f32, "params"), _flat(exp_avg, f32, "exp_avg"), _flat(exp_avg_sq, f32, "exp_avg_sq"), _flat(grads, _CODE, "grads")
+        if copies is not None:
+            _flat(copies, (torch.bfloat16,), "copies")
+        flat = []
+        for i in range(n):
+            p, g, c = params[i], grads[i], None if copies is None else copies[i]
+            size = p.numel()
+            _need(g.numel() == size and exp_avg[i].numel() == size and exp_avg_sq[i].numel() == size and
+                  (c is None or c.numel() == size), f"tensor {i}: parameter, gradient and states differ in size")
+            flat += (p.data_ptr(), exp_avg[i].data_ptr(), exp_avg_sq[i].data_ptr(), g.data_ptr(), 0 if c is None else c.data_ptr(), size,
+                     _CODE[g.dtype])
+        arr = (C.c_int64 * len(flat))(*flat)
+        by_tensor = isinstance(lr, torch.Tensor)
+        for t, dtype, what in ((step, torch.int32, "step"), (coef, torch.float32, "coef"), (lr if by_tensor else None, torch.float32, "lr")):
+            _need(t is None or t.numel() == 1, f"{what}: one element is needed")
+            _on(t, dtype, () if t is None else t.shape, what)
+        cfg = AdamwCfg(0.0 if by_tensor else lr, betas[0], betas[1], eps, weight_decay)
+        self._check(self.L.sol_adamw_step(self.handle, arr, n, C.byref(cfg), _ptr(step), _ptr(lr) if by_tensor else None, _ptr(coef),
+                                          _stream(stream)))
 
     def schedule_loglik(self, layers, head, tokens, targets, action_ids, nll_out=None, workspace=None, stream=None):
         """tokens/targets int32 [B][T]; action_ids int32 [B][G][T]. Returns nll float32 [B][G][T] (nats)."""

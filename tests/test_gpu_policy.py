@@ -1,0 +1,281 @@
+"""GPU parity of the policy loss and its gradient against the oracle (64 bits).
+
+Tolerances, derived: with t_j = (x_j - m) log2(e) / temperature, e_j = 2^t_j carries the rounding of a difference and of two products, i.e.
+ln2 * 3 * 2^-24 |t_j| relative, plus one step of 2^x; a sum of A terms at most min(A, 600) additions in one lane (and 16 across lanes)
+plus the errors of its terms; a coefficient at most 16 further roundings. A gradient is a sum of products of these, so its error is at
+most R * 2^-24 times the sum of the magnitudes it is made of (the oracle's `size`), R = 2 * 2.1 * max|t| + min(A, 600) + 48, plus half a
+step of its type. Elements whose |t| is over 60 have p < 2^-60 and are held to that share of their row."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2605_10875_amd import sol, synth
+
+from gpu_util import dev, host
+
+pytestmark = pytest.mark.gpu
+
+CLIP = (0.2, 0.28)
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = sol.Sol(synth.TINY, synth.TABLE_C1, dtype=sol.F32, max_positions=16)
+    yield c
+    c.close()
+
+
+def _rows(shape, dtype, ld, offset, rng, spread=2.0):
+    """Random logits as rows ld elements apart that begin `offset` elements into an allocation."""
+    B, G, T, A = shape
+    n = B * G * T
+    buf = torch.from_numpy(spread * rng.standard_normal(offset + n * ld)).to(dtype)
+    return buf.cuda()[offset:].as_strided((B, G, T, A), (G * T * ld, T * ld, ld, 1))
+
+
+def _case(B, G, T, A, dtype=torch.float32, pad=0, offset=0, kl="none", forbid=0, ragged=False, temperature=1.0, seed=0, spread=2.0):
+    rng = np.random.default_rng([seed, B, G, T, A])
+    x = _rows((B, G, T, A), dtype, A + pad, offset, rng, spread)
+    if forbid:
+        x[..., forbid - 1::forbid] = -np.inf
+    xh = host(x).astype(np.float64)
+    some = np.isfinite(xh)
+    ids = np.where(some, rng.random(xh.shape), -1.0).argmax(-1).astype(np.int32)
+    logp = np.array([oracle._log_softmax(xh[i], temperature)[ids[i]] for i in np.ndindex(B, G, T)]).reshape(B, G, T)
+    d = rng.uniform(-0.5, 0.5, (B, G, T))
+    for edge in (np.log1p(-CLIP[0]), np.log1p(CLIP[1])):               # the gradient jumps at the bounds
+        d = np.where(np.abs(d - edge) < 2e-3, edge + 4e-3, d)
+    kw = dict(adv=rng.standard_normal((B, G, T)).astype(np.float32), old_logp=(logp - d).astype(np.float32), clip=CLIP, entropy_coef=0.05,
+              temperature=temperature, scale=0.5, kl_coef=0.0 if kl == "none" else 0.1)
+    if kl == "logp":
+        kw["ref_logp"] = (logp + rng.uniform(-1.0, 1.0, (B, G, T))).astype(np.float32)
+    if kl == "logits":
+        ref = _rows((B, G, T, A), dtype, A + 2 * pad, (3 * offset) % 8, rng, spread)
+        if forbid:
+            ref[..., forbid - 1::forbid] = -np.inf
+        kw["ref_logits"] = ref
+    if ragged:
+        kw["eff"] = (rng.random((B, T)) < 0.7).astype(np.int32)
+        kw["eff"][0, 0] = 1
+    return x, ids, kw
+
+
+def _run(ctx, x, ids, kw, **more):
+    args = {k: v if not isinstance(v, np.ndarray) else dev(v) for k, v in kw.items()}
+    return ctx.policy_loss(x, dev(ids), **args, **more)
+
+
+def _oracle(x, ids, kw):
+    args = {k: host(v) if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+    return oracle.policy_loss(host(x), ids, **args)
+
+
+def _rel(x, kw):
+    xh = host(x).astype(np.float64)
+    t = np.where(np.isfinite(xh), xh.max(-1, keepdims=True) - np.where(np.isfinite(xh), xh, 0), 0.0) * 1.4427 / kw.get("temperature", 1.0)
+    return (4.2 * min(t.max(), 60.0) + min(x.shape[-1], 600) + 48) * 2.0 ** -24
+
+
+def _check(got, ref, x, kw, rel):
+    half = HALF[x.dtype]
+    tol = rel * ref["size"] + half * np.abs(ref["grad"]) + 2.0 ** -60 * ref["size"].max(-1, keepdims=True) + 1e-37
+    bad = np.abs(host(got["grad"]).astype(np.float64) - ref["grad"]) > tol
+    assert not bad.any(), (bad.sum(), np.argwhere(bad)[:3].tolist())
+    np.testing.assert_allclose(host(got["logp"]), ref["logp"], rtol=2.0 ** -23, atol=rel)
+    top = 1.0 + np.abs(kw["adv"]).max() * ref["ratio"].max() + np.abs(ref["stats"]).max()
+    np.testing.assert_allclose(host(got["stats"]), ref["stats"], rtol=2.0 ** -23, atol=4 * rel * top)
+    np.testing.assert_allclose(float(got["loss"]), ref["loss"], rtol=2.0 ** -23, atol=4 * rel * top)
+
+
+# rows of one element, within a lane, a few lanes, a wave, a workgroup, several of its steps; odd ones, and both sides of powers of two
+LENGTHS = [1, 2, 3, 7, 8, 9, 31, 64, 65, 80, 127, 129, 255, 257, 511, 513, 1000, 1025, 2047, 2050, 4001, 4097, 8191, 8200, 16387, 33000, 65541]
+
+
+@pytest.mark.parametrize("A", LENGTHS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["logp", "logits"])
+def test_every_length_against_the_oracle(ctx, A, dtype, kl):
+    x, ids, kw = _case(2, 2, 3, A, dtype, kl=kl, ragged=A % 3 == 0, seed=1)
+    got = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    _check(got, _oracle(x, ids, kw), x, kw, _rel(x, kw))
+
+
+@pytest.mark.parametrize("A,pad,offset", [(5, 3, 1), (64, 1, 3), (80, 16, 2), (333, 0, 5), (1000, 24, 0), (4001, 95, 0), (4000, 3, 7), (20001, 7, 1),
+                                          (128256, 0, 0), (131071, 2, 5), (140001, 1, 3)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["none", "logp", "logits"])
+def test_padded_and_unaligned_rows(ctx, A, pad, offset, dtype, kl):
+    x, ids, kw = _case(1, 2, 3, A, dtype, pad, offset, kl, forbid=7 if A > 7 else 0, temperature=1.3, seed=2)
+    got = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    _check(got, _oracle(x, ids, kw), x, kw, _rel(x, kw))
+
+
+@pytest.mark.parametrize("B,G,T,A", [(1, 1, 1, 64), (3, 5, 7, 27), (2, 16, 16, 64), (8, 32, 16, 80), (1, 3, 700, 16), (70, 1, 1, 9), (300, 2, 3, 4), (2, 8, 509, 64)])
+@pytest.mark.parametrize("mean", ["steps", "schedules"])
+def test_batches_and_means(ctx, B, G, T, A, mean):
+    x, ids, kw = _case(B, G, T, A, kl="logits", ragged=True, seed=3)
+    kw["mean"] = mean
+    got = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    _check(got, _oracle(x, ids, kw), x, kw, _rel(x, kw))
+
+
+def test_the_acting_policy_and_no_advantages(ctx):
+    x, ids, kw = _case(2, 2, 5, 33, seed=4)
+    for drop in (("old_logp",), ("adv",), ("old_logp", "adv")):
+        few = {k: v for k, v in kw.items() if k not in drop}
+        ref = _oracle(x, ids, few)
+        _check(_run(ctx, x, ids, few), ref, x, {**kw, **few}, _rel(x, kw))
+    assert ref["stats"][0] == 0.0
+
+
+@pytest.mark.parametrize("A", [5, 64, 700, 5000, 70001, 140001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["none", "logits"])
+def test_masks(ctx, A, dtype, kl):
+    """NaN in steps that do not count, rows without an allowed action, rows of the type's lowest value, one action left, a taken action
+    that is forbidden."""
+    x, ids, kw = _case(1, 2, 6, A, dtype, kl=kl, seed=5)
+    low = torch.finfo(dtype).min
+    kw["eff"] = np.array([[1, 0, 1, 1, 1, 1]], np.int32)
+    both = [x] + ([kw["ref_logits"]] if kl == "logits" else [])
+    for v in both:
+        v[:, :, 1] = np.nan
+        v[:, 0, 2] = -np.inf
+        v[:, 1, 2, 1:] = -np.inf
+        v[:, :, 3] = low
+        v[:, 0, 4, A // 2:] = low
+    ids[:, 1, 2] = 0
+    ids[:, 0, 4] = 0
+    x[:, 1, 4, A - 1] = -np.inf
+    ids[:, 1, 4] = A - 1                                               # p = 0: the ratio is 0
+    for k in ("adv", "old_logp"):
+        kw[k][:, :, 1] = np.nan
+    kw["adv"][:, 1, 4] = 1.0
+    with np.errstate(invalid="ignore"):
+        ref = _oracle(x, ids, kw)
+    got = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    assert host(got["logp"])[0, 0, 2] == -np.inf and host(got["logp"])[0, 1, 4] == -np.inf
+    assert not host(got["grad"])[:, :, 1].any() and not host(got["grad"])[:, 0, 2].any()
+    assert np.isfinite(host(got["grad"])).all() and np.isfinite(host(got["stats"])).all()
+    kw["adv"][:, :, 1] = 0
+    _check(got, ref, x, kw, _rel(x, kw) + 64 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("A", [6, 300, 9000, 140001])
+@pytest.mark.parametrize("what", [np.nan, np.inf])
+def test_a_row_that_is_not_a_distribution_is_nan_and_alone(ctx, A, what):
+    x, ids, kw = _case(1, 1, 5, A, seed=6)
+    clean = _run(ctx, x, ids, kw)
+    x[0, 0, 2, A // 3] = what
+    got = _run(ctx, x, ids, kw)
+    assert torch.isnan(got["grad"][0, 0, 2]).all() and torch.isnan(got["loss"]).all() and torch.isnan(got["logp"][0, 0, 2])
+    for t in (0, 1, 3, 4):
+        assert torch.equal(got["grad"][0, 0, t], clean["grad"][0, 0, t])
+
+
+@pytest.mark.parametrize("A,pad", [(9, 2), (64, 0), (1000, 8), (4001, 95), (70000, 0), (140001, 0)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["none", "logits"])
+def test_in_place_and_between_the_rows(ctx, A, pad, dtype, kl):
+    x, ids, kw = _case(1, 2, 5, A, dtype, pad, kl=kl, ragged=True, seed=7)
+    apart = _run(ctx, x, ids, kw)["grad"].clone()
+    whole = torch.as_strided(x, (10, A + pad), (A + pad, 1))
+    before = whole.clone()
+    got = _run(ctx, x, ids, kw, grad_out=x)
+    assert got["grad"] is x and torch.equal(x, apart)
+    assert torch.equal(whole[:9, A:], before[:9, A:])
+    loss_only = _run(ctx, before.as_strided(x.shape, x.stride()), ids, kw, want_grad=False)
+    assert loss_only["grad"] is None and torch.equal(loss_only["loss"], got["loss"]) and torch.equal(loss_only["logp"], got["logp"])
+
+
+def test_an_action_outside_the_range_counts_as_action_0_and_is_flagged(ctx):
+    x, ids, kw = _case(1, 2, 3, 11, seed=8)
+    ids[0, 1, 2] = 0
+    ref = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    for bad in (11, -1, 1 << 30):
+        ids[0, 1, 2] = bad
+        got = _run(ctx, x, ids, kw)
+        assert ctx.device_status() == sol.ERR_ACTION
+        assert torch.equal(got["grad"], ref["grad"])
+
+
+def test_no_effective_step_and_no_rows(ctx):
+    x, ids, kw = _case(2, 2, 3, 5, seed=9)
+    kw["eff"] = np.zeros((2, 3), np.int32)
+    got = _run(ctx, x, ids, kw)
+    assert float(got["loss"]) == 0.0 and not host(got["stats"]).any() and not host(got["grad"]).any() and not host(got["logp"]).any()
+    empty = ctx.policy_loss(torch.zeros((2, 0, 3, 5), device="cuda"), torch.zeros((2, 0, 3), dtype=torch.int32, device="cuda"))
+    assert empty["grad"].shape == (2, 0, 3, 5) and float(empty["loss"]) == 0.0
+
+
+@pytest.mark.parametrize("A", [27, 4001, 70001])
+def test_the_loss_by_differences(ctx, A):
+    """The gradient along a direction against differences of the loss itself: (l(h) - l(-h)) / 2h is off by h^2 / 6 times a third
+    derivative along v (at most 8 |v|_row^3 per row here) and by the loss's rounding, 2^-23 |l| / h."""
+    x, ids, kw = _case(1, 2, 8, A, kl="logits", seed=10, spread=1.0)
+    # past the bounds the loss has a corner, not near any of them along the line
+    v = torch.randn(x.shape, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    v /= v.flatten(3).norm(dim=-1, keepdim=True)
+    h = 2.0 ** -9
+    up, down = (float(_run(ctx, x + s * h * v, ids, kw, want_grad=False)["loss"].double()) for s in (1, -1))
+    got = _run(ctx, x, ids, kw)
+    along = float((got["grad"].double() * v.double()).sum())
+    assert abs((up - down) / (2 * h) - along) < 8 * h * h / 6 * 3 + 2.0 ** -23 * (abs(up) + 1) / h * 2
+
+
+def test_same_bits_again_on_another_stream_and_replayed(ctx):
+    cases = [_case(2, 3, 7, A, dt, kl=kl, ragged=True, seed=11) for A, dt, kl in ((80, torch.float32, "logp"), (5000, torch.bfloat16, "logits"),
+                                                                                 (140001, torch.float32, "none"))]
+    fixed = []
+    for x, ids, kw in cases:
+        args = {k: v if not isinstance(v, np.ndarray) else dev(v) for k, v in kw.items()}
+        fixed.append((x, dev(ids), args))
+    eager = [ctx.policy_loss(x, ids, **kw) for x, ids, kw in fixed]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        inside = [ctx.policy_loss(x, ids, **kw) for x, ids, kw in fixed]
+    passed = [ctx.policy_loss(x, ids, stream=side, **kw) for x, ids, kw in fixed]
+    torch.cuda.synchronize()
+    for a, b in zip(eager * 2, inside + passed):
+        assert all(torch.equal(a[k], b[k]) for k in a)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = [ctx.policy_loss(x, ids, **kw) for x, ids, kw in fixed]
+    for i in range(3):
+        for x, _, _ in fixed:
+            x.mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        again = [ctx.policy_loss(x, ids, **kw) for x, ids, kw in fixed]
+        torch.cuda.synchronize()
+        for a, b in zip(held, again):
+            assert all(torch.equal(a[k], b[k]) for k in a), i
+
+
+def test_refusals(ctx):
+    x, ids, kw = _case(1, 2, 3, 8, kl="logp", seed=12)
+
+    def bad(code, **change):
+        args = {**{k: dev(v) if isinstance(v, np.ndarray) else v for k, v in kw.items()}, **change}
+        with pytest.raises(sol.SolError) as e:
+            ctx.policy_loss(x, dev(ids), **args)
+        assert e.value.code == code, e.value
+
+    for change in (dict(clip=(-0.1, 0.2)), dict(clip=(1.1, 0.2)), dict(clip=(0.2, -1.0)), dict(kl_coef=-1.0), dict(kl_coef=float("nan")),
+                   dict(entropy_coef=float("inf")), dict(temperature=0.0), dict(temperature=float("nan")), dict(scale=float("inf")),
+                   dict(ref_logits=x.clone()), dict(ref_logp=None)):
+        bad(sol.ERR_INVALID_ARG, **change)
+    big = torch.zeros(3 * 6 * 8, device="cuda")
+    over = big.as_strided(x.shape, (2 * 3 * 16, 3 * 16, 16, 1))
+    with pytest.raises(sol.SolError) as e:
+        ctx.policy_loss(big[8:].as_strided(x.shape, (48, 24, 8, 1)), dev(ids), grad_out=over)
+    assert e.value.code == sol.ERR_INVALID_ARG and "overlap" in str(e.value)
+    assert ctx.device_status() == sol.OK

@@ -1,0 +1,282 @@
+"""GPU parity of the gradient norm with clipping and of AdamW against the oracle (64 bits), over lists of ragged, unaligned, mixed tensors.
+
+Tolerances, derived. Norm: squares and sums in 64 bits, rounded once: 2^-24 relative (and 2^-24 for the test's own value in fp32). A clipped
+gradient: the coefficient's rounding, the product's, half a step of the type. AdamW: a moment has at most 5 roundings of its
+two terms' magnitudes; the update's factor at most 12 further ones."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2605_10875_amd import sol, synth
+
+from gpu_util import host
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = sol.Sol(synth.TINY, synth.TABLE_C1, dtype=sol.F32, max_positions=16)
+    yield c
+    c.close()
+
+
+def _split(sizes, dtype, rng, scale=1.0, gap=1, positive=False):
+    """Views into one allocation, `gap` elements apart, so that most of them are not aligned to more than their elements."""
+    n = sum(sizes) + gap * (len(sizes) + 1)
+    v = scale * rng.standard_normal(n)
+    flat = torch.from_numpy(np.abs(v) if positive else v).to(dtype).cuda()
+    out, at = [], gap
+    for s in sizes:
+        out.append(flat[at:at + s])
+        at += s + gap
+    return flat, out
+
+
+LISTS = [[1], [0, 5, 0], [7, 1, 64, 1000], [4096], [4095, 4097, 8192, 3], [100003], [300000, 1, 1 << 20], [5] * 161, [33, 70001] * 90, [257] * 400]
+
+
+@pytest.mark.parametrize("sizes", LISTS, ids=[f"{len(s)}x{max(s)}" for s in LISTS])
+@pytest.mark.parametrize("types", ["fp32", "bf16", "mixed"])
+@pytest.mark.parametrize("gap", [0, 1])
+def test_norm_and_clip(ctx, sizes, types, gap):
+    rng = np.random.default_rng(len(sizes) + sizes[0])
+    fa, a = _split(sizes, torch.float32, rng, 0.3, gap)
+    fb, b = _split(sizes, torch.bfloat16, rng, 0.3, gap)
+    ts = a if types == "fp32" else b if types == "bf16" else [v for p in zip(a, b) for v in p]
+    before = [t.clone() for t in ts]
+    whole = [fa.clone(), fb.clone()]
+    norm0 = oracle.grad_clip([host(t) for t in ts], 1.0)[0]
+    for max_norm in (norm0 * 0.37, norm0 * 1.5, float("inf")):
+        norm, coef, ref = oracle.grad_clip([host(t) for t in before], max_norm)
+        for scale in (False, True):
+            n, c = ctx.grad_clip(ts, max_norm, scale=scale)
+            assert abs(float(n) - norm) <= 2 * EPS * norm and abs(float(c) - coef) <= 2 * EPS * coef
+            for t, was, r in zip(ts, before, ref):
+                if not scale or coef == 1.0:
+                    assert torch.equal(t, was)
+                else:
+                    tol = (3 * EPS + HALF[t.dtype]) * np.abs(r) + (2.0 ** -149 if t.dtype == torch.float32 else 2.0 ** -133)
+                    assert (np.abs(host(t).astype(np.float64) - r) <= tol).all()
+        for t, was in zip(ts, before):
+            t.copy_(was)
+    ctx.grad_clip(ts, norm0 * 0.37)
+    if gap:                                                            # what lies between the tensors
+        mark = [torch.zeros_like(f, dtype=torch.bool) for f in (fa, fb)]
+        for m, f, views in zip(mark, (fa, fb), (a, b)):
+            for v in views:
+                o = v.storage_offset()
+                m[o:o + v.numel()] = True
+        assert torch.equal(fa[~mark[0]], whole[0][~mark[0]]) and torch.equal(fb[~mark[1]], whole[1][~mark[1]])
+
+
+def test_an_empty_list_and_large_and_tiny_values(ctx):
+    n, c = ctx.grad_clip([], 1.0)
+    assert float(n) == 0.0 and float(c) == 1.0
+    big = torch.full((5000,), 1e30, device="cuda")                    # squares are beyond 32 bits
+    n, c = ctx.grad_clip([big], 1e31)
+    assert np.isclose(float(n), np.sqrt(5000) * np.float32(1e30), rtol=1e-6)
+    assert np.isclose(float(torch.linalg.vector_norm(big.double())), 1e31, rtol=1e-6)
+    tiny = torch.full((5000,), 1e-30, device="cuda")
+    assert np.isclose(float(ctx.grad_clip([tiny], 1.0)[0]), np.sqrt(5000) * 1e-30, rtol=1e-6)
+
+
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+def test_a_norm_that_is_not_finite_leaves_everything(ctx, what):
+    g = torch.randn(70000, device="cuda")
+    g[4711] = what
+    was = g.clone()
+    n, c = ctx.grad_clip([g], 1.0)
+    assert not np.isfinite(float(n)) and np.isnan(float(c))
+    assert torch.equal(g.view(torch.int32), was.view(torch.int32))
+    p, m, v = (torch.randn(70000, device="cuda").abs() for _ in range(3))
+    held = [t.clone() for t in (p, m, v)]
+    ctx.adamw_step([p], [g], [m], [v], torch.ones(1, dtype=torch.int32, device="cuda"), 1e-3, coef=c)
+    assert all(torch.equal(a, b) for a, b in zip((p, m, v), held))
+    assert ctx.device_status() == sol.OK
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 9], [4096, 3, 4097], [1 << 20, 77], [11] * 57, [33, 5001] * 80], ids=lambda s: f"{len(s)}x{max(s)}")
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("gap", [0, 1, 3])
+def test_adamw_over_some_updates(ctx, sizes, dtype, gap):
+    rng = np.random.default_rng(len(sizes) + gap)
+    kw = dict(betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1)
+    fp, p = _split(sizes, torch.float32, rng, 1.0, gap)
+    _, m = _split(sizes, torch.float32, rng, 0.1, gap)
+    _, v = _split(sizes, torch.float32, rng, 0.1, gap, positive=True)
+    _, g = _split(sizes, dtype, rng, 0.3, gap)
+    _, copy = _split(sizes, torch.bfloat16, rng, 1.0, gap)
+    outside = fp.clone()
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    coef = torch.full((1,), 0.625, device="cuda")
+    for t in (1, 2, 1000):
+        step.fill_(t)
+        ref = [oracle.adamw_step(host(a), host(b), host(c), host(d), t, 1e-2, coef=0.625, **kw) for a, b, c, d in zip(p, g, m, v)]
+        was = [[host(x).astype(np.float64) for x in y] for y in (p, m, v, g)]
+        ctx.adamw_step(p, g, m, v, step, 1e-2, coef=coef, copies=copy if t != 2 else None, **kw)
+        for i in range(len(sizes)):
+            rp, rm, rv = ref[i]
+            gi = 0.625 * np.abs(was[3][i])
+            tm = 6 * EPS * (0.9 * np.abs(was[1][i]) + 0.1 * gi) + 1e-44
+            tv = 6 * EPS * (0.95 * was[2][i] + 0.05 * gi ** 2) + 1e-44
+            denom = np.sqrt(rv / (1 - 0.95 ** t)) + 1e-8
+            change = 1e-2 / (1 - 0.9 ** t) / denom
+            tp = 3 * EPS * np.abs(was[0][i]) + change * (tm + np.abs(rm) * (12 * EPS + tv / np.maximum(rv, 1e-40)))
+            assert (np.abs(host(m[i]) - rm) <= tm).all() and (np.abs(host(v[i]) - rv) <= tv).all()
+            assert (np.abs(host(p[i]) - rp) <= tp).all()
+            if t != 2:
+                assert torch.equal(copy[i], p[i].to(torch.bfloat16))
+    if gap:
+        mask = torch.ones_like(fp, dtype=torch.bool)
+        for x in p:
+            mask[x.storage_offset():x.storage_offset() + x.numel()] = False
+        assert torch.equal(fp[mask], outside[mask])
+    assert ctx.device_status() == sol.OK
+
+
+def _states(n, dtype=torch.float32, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    p, g, m, v = (torch.randn(n, generator=gen, device="cuda") for _ in range(4))
+    return p, g.to(dtype), 0.1 * m, 0.01 * v.square()
+
+
+def test_learning_rate_on_the_device_and_step_below_1(ctx):
+    step = torch.full((1,), 3, dtype=torch.int32, device="cuda")
+    a, b = _states(9999), _states(9999)
+    ctx.adamw_step([a[0]], [a[1]], [a[2]], [a[3]], step, 0.125)
+    ctx.adamw_step([b[0]], [b[1]], [b[2]], [b[3]], step, torch.full((1,), 0.125, device="cuda"))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    step.zero_()
+    assert ctx.device_status() == sol.OK
+    ctx.adamw_step([a[0]], [a[1]], [a[2]], [a[3]], step, 0.125)
+    assert ctx.device_status() == sol.ERR_INVALID_ARG
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_gradient_may_serve_two_parameters(ctx):
+    step = torch.ones(1, dtype=torch.int32, device="cuda")
+    a, b = _states(5000, seed=1), _states(5000, seed=2)
+    alone = [t.clone() for t in b]
+    ctx.adamw_step([alone[0]], [a[1]], [alone[2]], [alone[3]], step, 1e-2)
+    ctx.adamw_step([a[0], b[0]], [a[1], a[1]], [a[2], b[2]], [a[3], b[3]], step, 1e-2)
+    assert torch.equal(b[0], alone[0]) and torch.equal(b[3], alone[3])
+
+
+def test_refusals(ctx):
+    step = torch.ones(1, dtype=torch.int32, device="cuda")
+    p, g, m, v = _states(64)
+
+    def bad(fn, word=""):
+        with pytest.raises(sol.SolError) as e:
+            fn()
+        assert e.value.code == sol.ERR_INVALID_ARG and word in str(e.value), e.value
+
+    for norm in (0.0, -1.0, float("nan")):
+        bad(lambda: ctx.grad_clip([g], norm))
+    bad(lambda: ctx.grad_clip([g], 1.0, eps=-1.0))
+    bad(lambda: ctx.grad_clip([g[:40], g[39:]], 1.0), "overlap")
+    bad(lambda: ctx.grad_clip([g, g], 1.0), "overlap")
+    ctx.grad_clip([g, g], 1.0, scale=False)                            # reading twice is no harm
+    bad(lambda: ctx.adamw_step([p], [g], [m], [m], step, 1e-3), "overlap")
+    bad(lambda: ctx.adamw_step([p, p], [g, g], [m, m], [v, v], step, 1e-3), "overlap")
+    bad(lambda: ctx.adamw_step([p], [m], [m], [v], step, 1e-3), "overlap")
+    bad(lambda: ctx.adamw_step([p[:32]], [p[31:63]], [m[:32]], [v[:32]], step, 1e-3), "overlap")
+    for kw in (dict(lr=-1.0), dict(lr=float("nan")), dict(lr=1e-3, betas=(1.0, 0.9)), dict(lr=1e-3, betas=(0.9, -0.1)), dict(lr=1e-3, eps=-1.0),
+               dict(lr=1e-3, weight_decay=float("inf"))):
+        bad(lambda: ctx.adamw_step([p], [g], [m], [v], step, **kw))
+    with pytest.raises(ValueError):
+        ctx.adamw_step([p], [g[:5]], [m], [v], step, 1e-3)
+    tiny = (sol.C.c_int64 * 3)(g.data_ptr(), 64, 0)
+    out = torch.zeros(2, device="cuda")
+    assert ctx.L.sol_grad_clip(ctx.handle, tiny, 1, 1.0, 0.0, 0, out.data_ptr(), out[1:].data_ptr(), out.data_ptr(), 8, None) == sol.ERR_WORKSPACE
+    assert ctx.device_status() == sol.OK
+
+
+def test_captured_norm_clip_and_update(ctx):
+    """One graph of norm, clip and two updates, its step advanced inside, against the same calls made one by one."""
+    sizes = [1000, 3, 70001] + [50] * 200
+    rng = np.random.default_rng(5)
+    sets = []
+    for _ in range(2):
+        rng = np.random.default_rng(5)
+        sets.append([_split(sizes, dt, rng, 0.1, 1, pos)[1] for dt, pos in ((torch.float32, False), (torch.bfloat16, False), (torch.float32, False),
+                                                                               (torch.float32, True))] + [torch.zeros(1, dtype=torch.int32, device="cuda")])
+
+    def update(s):
+        p, g, m, v, step = s
+        step.add_(1)
+        norm, coef = ctx.grad_clip(g, 0.5, scale=False)
+        ctx.adamw_step(p, g, m, v, step, 1e-3, coef=coef, weight_decay=0.01)
+        return norm
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = update(sets[0])
+    for i in range(4):
+        for s in sets:
+            for t in s[1]:
+                t.mul_(1.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = update(sets[1])
+        torch.cuda.synchronize()
+        assert torch.equal(held, norm), i
+        for k in (0, 2, 3):
+            assert all(torch.equal(a, b) for a, b in zip(sets[0][k], sets[1][k])), i
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_a_policy_is_trained_on_rewards(ctx, dtype):
+    """As a trainer uses them together: likelihoods -> advantages -> loss and gradient -> the network's own backward -> clip -> update,
+    three updates of a small policy, against the oracle's formulas on the same network in 64 bits on the CPU."""
+    B, G, T, d = 2, 4, 9, 24
+    A = len(synth.TABLE_C1)
+    rng = np.random.default_rng(77)
+    nll = rng.uniform(0.2, 8.0, (B, G, T)).astype(np.float32)
+    ids = rng.integers(0, A, (B, G, T)).astype(np.int32)
+    targets = rng.uniform(0.3, 1.0, (B, 3)).astype(np.float32)
+    feats = rng.standard_normal((B, G, T, d)).astype(np.float32)
+    eff = np.ones((B, T), np.int32)
+    eff[1, 6:] = 0
+    w0 = (0.2 * rng.standard_normal((A, d))).astype(np.float32)
+    adv = ctx.reward_advantages(*(torch.from_numpy(v).cuda() for v in (nll, ids, targets)), (1.0, 0.5, 0.25), 0.02, 0.9,
+                                eff=torch.from_numpy(eff).cuda())["adv"]
+    x = torch.from_numpy(feats).cuda().to(dtype)
+    master = torch.from_numpy(w0).cuda()
+    weight = master.to(dtype, copy=True).requires_grad_(True)
+    m, v, step = torch.zeros_like(master), torch.zeros_like(master), torch.zeros(1, dtype=torch.int32, device="cuda")
+    first = None
+    ow, om, ov = master.double().cpu().numpy(), np.zeros((A, d)), np.zeros((A, d))
+    common = dict(clip=(0.2, 0.28), kl_coef=0.04, entropy_coef=0.05, temperature=1.3)
+    for t in range(1, 4):
+        logits = x @ weight.t()
+        if first is None:                                              # the acting policy is the reference too
+            first = ctx.policy_loss(logits.detach(), torch.from_numpy(ids).cuda(), temperature=1.3, want_grad=False)["logp"]
+        out = ctx.policy_loss(logits.detach(), torch.from_numpy(ids).cuda(), adv, old_logp=first, ref_logp=first,
+                              eff=torch.from_numpy(eff).cuda(), **common)
+        logits.backward(out["grad"])
+        lh = host(logits)
+        ref = oracle.policy_loss(lh, ids, host(adv), old_logp=host(first), ref_logp=host(first), eff=eff, **common)
+        np.testing.assert_allclose(float(out["loss"]), ref["loss"], rtol=1e-5, atol=1e-5)
+        g = weight.grad.contiguous()
+        go = host(g).astype(np.float64)                                # (torch's own product is not under test)
+        norm, coef = ctx.grad_clip([g], 0.05, scale=False)
+        step.add_(1)
+        copies = None if dtype == torch.float32 else [weight.data]
+        ctx.adamw_step([master], [g], [m], [v], step, 1e-2, coef=coef, copies=copies)
+        n, c, _ = oracle.grad_clip([go], 0.05)
+        ow, om, ov = oracle.adamw_step(ow, go, om, ov, t, 1e-2, coef=c)
+        assert abs(float(norm) - n) <= 2 * EPS * n
+        # per update: 16 roundings of a step of 1e-2 * |m| / sqrt(v) (below 1e-2 * 3.2 in the first three) and of the parameter
+        np.testing.assert_allclose(host(master), ow, rtol=t * 4 * EPS, atol=t * 16 * EPS * 0.032 + 1e-8)
+        weight.grad = None
+        if dtype == torch.float32:
+            weight.data.copy_(master)
+        else:
+            assert torch.equal(weight.data, master.to(dtype))
+    assert ctx.device_status() == sol.OK
