@@ -18,12 +18,14 @@ constexpr int PL_BLOCK = 256;
 constexpr int PL_GRID = 2048;                                       // workgroups of the rows' kernel at most
 constexpr float PL_LOG2E = 1.44269504088896341f;
 constexpr double PL_LN2 = 0.693147180559945309;
+constexpr float PL_LOWEST = -3.402823466e38f;                       // below every finite logit's maximum: no NaN from -inf - -inf
+constexpr float PL_ZERO = -1e4f;                                    // 2^t is zero from here on: bounds t where t times zero is taken
 
 struct PolicyScalars { double inv_temp, log_lo, log_hi, lo, hi, kl, ent, scale; };
 
 // what a row needs besides its sums
 struct PolicyRow { int a; float adv, old, ref; double w; };
-struct PolicySums { double S, Sr; float U, K, ln_diff; };
+struct PolicySums { float S, Sr, U, K; };
 struct PolicyCoef { float alpha, gamma, kappa, hot, logp, pg, kl, ent, clipped; };
 
 // w[b] = share of an effective step of input b in the mean (0: the input has none)
@@ -75,34 +77,56 @@ __device__ __forceinline__ float policy_kl(float u)
     return fabsf(u) < 0.5f ? s * u * u : expf(u) - u - 1.f;
 }
 
+// log x for 2^-1000 < x < 2^1000: mantissa in [sqrt 1/2, sqrt 2), log f = 2 artanh((f - 1) / (f + 1)), whose argument is at most
+// 0.1716, so that the first term left out (s^17) is below 1e-14. A third of the instructions of the library's.
+__device__ __forceinline__ double policy_log(double x)
+{
+    double f = __builtin_amdgcn_frexp_mant(x);
+    int k = __builtin_amdgcn_frexp_exp(x);
+    if (f < 0.70710678118654752) { f *= 2.0; --k; }
+    const double d = f + 1.0;
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    const double s = (f - 1.0) * r, q = s * s;
+    double p = 2.0 / 15.0;
+    p = __builtin_fma(p, q, 2.0 / 13.0);
+    p = __builtin_fma(p, q, 2.0 / 11.0);
+    p = __builtin_fma(p, q, 2.0 / 9.0);
+    p = __builtin_fma(p, q, 2.0 / 7.0);
+    p = __builtin_fma(p, q, 2.0 / 5.0);
+    p = __builtin_fma(p, q, 2.0 / 3.0);
+    p = __builtin_fma(p, q, 2.0);
+    return __builtin_fma((double)k, PL_LN2, s * p);
+}
+
 // The row's loss terms and the coefficients of its gradient from its sums. xa: the taken action's logit minus the maximum.
-// The ratio's bounds are tested on the logarithm in 64 bits: a gradient is not continuous there.
+// The ratio's bounds are tested on its logarithm in 64 bits: a gradient is not continuous there.
 __device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const PolicyRow &r, const PolicySums &s, float xa,
                                                  bool has_old, bool has_ref, bool exact_kl)
 {
     PolicyCoef c;
-    const double logS = log(s.S), logp = (double)xa * pc.inv_temp - logS;
+    const double logS = policy_log((double)s.S), logp = (double)xa * pc.inv_temp - logS;
     const double d = has_old ? logp - (double)r.old : 0.0;
     const float A = r.adv, rho = expf((float)d);
     const bool clipped = (A > 0.f && d > pc.log_hi) || (A < 0.f && d < pc.log_lo);
     c.logp = (float)logp;
     c.pg = clipped ? -(A > 0.f ? (float)pc.hi : (float)pc.lo) * A : -rho * A;
     float G = clipped ? 0.f : -rho * A;
-    const float beta = (float)pc.kl, ln2 = (float)PL_LN2, inv = (float)(1.0 / s.S), u_mean = ln2 * s.U * inv;
+    const float beta = (float)pc.kl, ln2 = (float)PL_LN2, inv = 1.f / s.S, u_mean = ln2 * s.U * inv;
     c.ent = (float)(logS - (double)u_mean);
     c.kl = 0.f;
     float k_mean = 0.f;
     if (exact_kl) {
         k_mean = ln2 * s.K * inv;
-        c.kl = (float)((double)k_mean - (logS - log(s.Sr)));
+        c.kl = (float)((double)k_mean - (logS - policy_log((double)s.Sr)));
     } else if (has_ref) {
         const float u = (float)((double)r.ref - logp);
         c.kl = policy_kl(u);
         G -= beta * (u + c.kl);                                     // 1 - exp(u)
     }
     c.clipped = clipped ? 1.f : 0.f;
-    const double wt = r.w * pc.scale * pc.inv_temp;
-    const float w = (float)wt, ent = (float)pc.ent;
+    const float w = (float)(r.w * pc.scale * pc.inv_temp), ent = (float)pc.ent;
     c.hot = w * G;
     c.alpha = -w * (G + ent * u_mean + (exact_kl ? beta * k_mean : 0.f)) * inv;
     c.gamma = w * ent * ln2 * inv;
@@ -110,64 +134,306 @@ __device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const 
     return c;
 }
 
-// One workgroup per row, rows strided over the grid. Three passes over the row: maximum, sums, gradient.
-template <class T, bool EXACT>
-__global__ void __launch_bounds__(PL_BLOCK)
-k_policy_rows(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
+// ---- a row's elements in 16-byte pieces -------------------------------------------------------------------------
+// Piece i of a row covers elements V i - mis .. V i - mis + V - 1, mis being the row's distance from a 16-byte boundary in elements,
+// so that every piece inside the row is one aligned access whatever the row's length and start are. Elements outside are -inf.
+template <class T> __device__ __forceinline__ int policy_mis(const T *x) { return (int)(((uintptr_t)x & 15) / sizeof(T)); }
+template <class T> __device__ __forceinline__ uint4 policy_none()
 {
-    __shared__ float red[PL_BLOCK / 64];
-    const T *const X = (const T *)q.logits, *const Y = (const T *)q.ref_logits;
-    T *const D = (T *)q.grad;
+    const uint32_t w = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    return make_uint4(w, w, w, w);
+}
+template <class T> __device__ __forceinline__ uint4 policy_edge(const T *x, int j, int A)
+{
+    uint32_t w[4];
+    constexpr int V = Vec16<T>::N;
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = (unsigned)(j + i) < (unsigned)A ? ((const uint32_t *)x)[j + i] : 0xFF800000u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            const uint32_t lo = (unsigned)(j + i) < (unsigned)A ? ((const uint16_t *)x)[j + i] : 0xFF80u;
+            const uint32_t hi = (unsigned)(j + i + 1) < (unsigned)A ? ((const uint16_t *)x)[j + i + 1] : 0xFF80u;
+            w[i / 2] = lo | hi << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <class T> __device__ __forceinline__ void policy_unpack(uint4 raw, float *f)
+{
+    Vec16<T> v;
+    v.raw = __builtin_bit_cast(decltype(v.raw), raw);
+    v.unpack(f);
+}
+template <class T> __device__ __forceinline__ void policy_put(T *d, const float *f, int j, int A, bool vec)
+{
+    constexpr int V = Vec16<T>::N;
+    if (vec && j >= 0 && j + V <= A) {
+        if (sizeof(T) == 4) *(float4 *)(d + j) = make_float4(f[0], f[1], f[2], f[3]);
+        else *(uint4 *)(d + j) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4 % V], f[5 % V]), pack_bf16x2(f[6 % V], f[7 % V]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) if ((unsigned)(j + i) < (unsigned)A) st(d + j + i, f[i]);
+    }
+}
+
+// ---- sums over the LANES lanes of a row: inside a wave, or over the waves of the workgroup ---------------------------
+template <int LANES, class Op> __device__ __forceinline__ float lanes_reduce(float v, Op op)
+{
+    auto dpp = [&](auto ctrl) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    if (LANES >= 2) v = op(v, dpp(std::integral_constant<int, 0xB1>{}));     // neighbour
+    if (LANES >= 4) v = op(v, dpp(std::integral_constant<int, 0x4E>{}));     // other pair of the four
+    if (LANES >= 8) v = op(v, dpp(std::integral_constant<int, 0x141>{}));    // other four of the eight
+    if (LANES >= 16) v = op(v, dpp(std::integral_constant<int, 0x140>{}));   // other eight of the sixteen
+    if (LANES >= 32) v = op(v, __shfl_xor(v, 16, 64));
+    if (LANES >= 64) v = op(v, __shfl_xor(v, 32, 64));
+    return v;
+}
+struct OpMaxF { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+
+// N values at once; slot: LDS of this use alone. One barrier: a slot is written again only behind the other slot's barrier.
+template <int LANES, int N, class Op> __device__ __forceinline__ void row_reduce(float (&v)[N], Op op, float (*slot)[16])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lanes_reduce<(LANES > 64 ? 64 : LANES)>(v[i], op);
+    if (LANES > 64) {
+        constexpr int W = LANES / 64;
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) slot[i][w] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = lanes_reduce<(W < 2 ? 2 : W)>(slot[i][lane & (W - 1)], op);
+    }
+}
+
+// A row's share of the loss, and its inputs but the logits
+__device__ __forceinline__ double policy_weight(const PolicyArgs &q, int row, double w_all, const double *w_in)
+{
+    if (!q.eff) return w_all;
+    const int b = row / (q.G * q.T), t = row % q.T;
+    return q.eff[(int64_t)b * q.T + t] ? w_in[b] : 0.0;
+}
+__device__ __forceinline__ PolicyRow policy_inputs(const PolicyArgs &q, int row, double w, bool first)
+{
+    PolicyRow r;
+    r.a = q.ids[row];
+    if (r.a < 0 || r.a >= q.A) { r.a = 0; if (first) atomicOr(q.flags, FLAG_BAD_ACTION); }
+    r.adv = q.adv ? q.adv[row] : 0.f;
+    r.old = q.old_logp ? q.old_logp[row] : 0.f;
+    r.ref = q.ref_logp ? q.ref_logp[row] : 0.f;
+    r.w = w;
+    return r;
+}
+
+template <class T, bool EXACT> struct PolicyPiece {
+    static constexpr int V = Vec16<T>::N;
+    static __device__ __forceinline__ void max(uint4 rx, uint4 ry, float (&m)[2])
+    {
+        float f[V];
+        policy_unpack<T>(rx, f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) m[0] = fmaxf(m[0], f[i]);
+        if (EXACT) {
+            policy_unpack<T>(ry, f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) m[1] = fmaxf(m[1], f[i]);
+        }
+    }
+    // s: S, U, S', K
+    static __device__ __forceinline__ void sums(uint4 rx, uint4 ry, float m, float mr, float k, float (&s)[4])
+    {
+        float f[V], g[V];
+        policy_unpack<T>(rx, f);
+        if (EXACT) policy_unpack<T>(ry, g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float t = (f[i] - m) * k, e = __builtin_amdgcn_exp2f(t);
+            s[0] += e;
+            s[1] = __builtin_fmaf(e, fmaxf(t, PL_ZERO), s[1]);
+            if (EXACT) {
+                const float r = (g[i] - mr) * k;
+                s[2] += __builtin_amdgcn_exp2f(r);
+                s[3] += e > 0.f ? e * (t - r) : 0.f;
+            }
+        }
+    }
+    static __device__ __forceinline__ void grad(uint4 rx, uint4 ry, float m, float mr, float k, const PolicyCoef &c, int at, float (&o)[V])
+    {
+        float f[V], g[V];
+        policy_unpack<T>(rx, f);
+        if (EXACT) policy_unpack<T>(ry, g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float t = (f[i] - m) * k, e = __builtin_amdgcn_exp2f(t);
+            float h = __builtin_fmaf(c.gamma, fmaxf(t, PL_ZERO), c.alpha);
+            if (EXACT) h += e > 0.f ? c.kappa * (t - (g[i] - mr) * k) : 0.f;
+            o[i] = e * h;
+        }
+        if ((unsigned)at < (unsigned)V)                             // the action taken is among them
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] += i == at ? c.hot : 0.f;
+    }
+};
+
+__device__ __forceinline__ double lanes_sum_f64(double v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// A row in the registers of LANES lanes, CH pieces of 16 bytes per lane: it is read once, all lanes wait for nothing but the row's
+// maximum and its sums. LANES <= 64: several rows per wave, side by side, no LDS.
+template <class T, bool EXACT, int LANES, int CH>
+__global__ void __launch_bounds__(LANES > PL_BLOCK ? LANES : PL_BLOCK)
+k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
+{
+    using P = PolicyPiece<T, EXACT>;
+    constexpr int V = P::V, BLOCK = LANES > PL_BLOCK ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
+    __shared__ float s_max[2][16], s_sum[4][16];
+    __shared__ double s_part[BLOCK / 64][4];
+    const int tid = threadIdx.x, lane = tid % LANES, A = q.A;
+    const float k = (float)pc.inv_temp * PL_LOG2E;
+    const int rows = q.B * q.G * q.T, used = (A + V - 1 + LANES * V - 1) / (LANES * V);     // pieces per lane, wherever the row begins
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < rows; first += (int64_t)gridDim.x * ROWS) {
+        const int64_t at = first + tid / LANES;
+        const bool there = at < rows;                               // (the same for all lanes of a row, as live is)
+        const int row = (int)(there ? at : rows - 1);
+        const double w = there ? policy_weight(q, row, w_all, w_in) : 0.0;
+        const bool live = w != 0.0;
+        const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
+        const int mis = policy_mis(x);
+        const bool same = EXACT && policy_mis(y) == mis;
+        uint4 rx[CH], ry[EXACT ? CH : 1];
+        auto pieces = [&](auto f) {                                 // f(piece, its first element), all of them in registers
+            static_for<CH>([&](auto c) { if (c < used) f(c, ((int)c * LANES + lane) * V - mis); });
+        };
+        pieces([&](auto c, int j) {
+            const bool whole = live && j >= 0 && j + V <= A;
+            rx[c] = whole ? *(const uint4 *)(x + j) : policy_none<T>();
+            if (EXACT) ry[EXACT ? (int)c : 0] = whole && same ? *(const uint4 *)(y + j) : policy_none<T>();
+        });
+        PolicyRow r{};
+        float xa = 0.f;
+        if (live) {
+            r = policy_inputs(q, row, w, lane == 0);
+            xa = ld(x + r.a);
+        }
+        pieces([&](auto c, int j) {
+            const bool part = live && j < A, cut = j < 0 || j + V > A;
+            if (part && cut) rx[c] = policy_edge(x, j, A);
+            if (EXACT && part && (cut || !same)) ry[EXACT ? (int)c : 0] = policy_edge(y, j, A);
+        });
+        float m[2] = {PL_LOWEST, PL_LOWEST}, s[4] = {0.f, 0.f, 0.f, 0.f};
+        pieces([&](auto c, int) { P::max(rx[c], ry[EXACT ? (int)c : 0], m); });
+        if (EXACT) row_reduce<LANES>(m, OpMaxF(), s_max);
+        else { float one[1] = {m[0]}; row_reduce<LANES>(one, OpMaxF(), s_max); m[0] = one[0]; }
+        pieces([&](auto c, int) { P::sums(rx[c], ry[EXACT ? (int)c : 0], m[0], m[1], k, s); });
+        if (EXACT) row_reduce<LANES>(s, OpAddF(), s_sum);
+        else { float two[2] = {s[0], s[1]}; row_reduce<LANES>(two, OpAddF(), s_sum); s[0] = two[0]; s[1] = two[1]; }
+        PolicyCoef c = policy_row(pc, r, PolicySums{s[0], s[2], s[1], s[3]}, xa - m[0], q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        const bool dead = !live || s[0] == 0.f;                     // not an effective step, or no action allowed
+        if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
+        if (there && lane == 0) {
+            if (q.logp) q.logp[row] = c.logp;
+            sum[0] += w * (double)c.pg;
+            sum[1] += w * (double)c.kl;
+            sum[2] += w * (double)c.ent;
+            sum[3] += w * (double)c.clipped;
+        }
+        if (there && q.grad) {
+            T *const d = (T *)q.grad + (int64_t)row * q.grad_ld;
+            const bool vec = policy_mis(d) == mis;
+            pieces([&](auto i, int j) {
+                float o[V];
+                P::grad(rx[i], ry[EXACT ? (int)i : 0], m[0], m[1], k, c, r.a - j, o);
+                if (j < A) policy_put(d, o, j, A, vec);
+            });
+        }
+    }
+    const int wave = tid >> 6;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum[i] = lanes_sum_f64(sum[i]);
+        if ((tid & 63) == 0) s_part[wave][i] = sum[i];
+    }
+    __syncthreads();
+    if (tid < 4) {
+        double v = 0.0;
+#pragma unroll
+        for (int i = 0; i < BLOCK / 64; ++i) v += s_part[i][tid];
+        partial[4 * (int64_t)blockIdx.x + tid] = v;
+    }
+}
+
+// A row that does not fit: one workgroup, two sweeps. The first keeps a running maximum per lane, its sums scaled anew where the
+// maximum of the next PIECES pieces is larger; the second reads the row again, from the caches where the rows in flight fit them.
+constexpr int PL_STREAM = 512, PL_PIECES = 4;
+template <class T, bool EXACT>
+__global__ void __launch_bounds__(PL_STREAM)
+k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
+{
+    using P = PolicyPiece<T, EXACT>;
+    constexpr int V = P::V;
+    __shared__ float s_max[2][16], s_sum[4][16];
     const int tid = threadIdx.x, A = q.A;
-    const float k = (float)(pc.inv_temp) * PL_LOG2E;
+    const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int b = row / (q.G * q.T), t = row % q.T;
-        const double w = !q.eff ? w_all : q.eff[(int64_t)b * q.T + t] ? w_in[b] : 0.0;
-        T *const dst = D ? D + (int64_t)row * q.grad_ld : nullptr;
-        if (w == 0.0) {                                             // not an effective step: the row is not read
-            if (dst) for (int j = tid; j < A; j += PL_BLOCK) st(dst + j, 0.f);
-            if (tid == 0 && q.logp) q.logp[row] = 0.f;
-            continue;
-        }
-        const T *const x = X + (int64_t)row * q.ld, *const y = EXACT ? Y + (int64_t)row * q.ref_ld : nullptr;
-        float m = -3.402823466e38f, mr = -3.402823466e38f;
-        for (int j = tid; j < A; j += PL_BLOCK) {
-            m = fmaxf(m, ld(x + j));
-            if (EXACT) mr = fmaxf(mr, ld(y + j));
-        }
-        m = block_max<PL_BLOCK>(m, red);
-        if (EXACT) mr = block_max<PL_BLOCK>(mr, red);
-        float S = 0.f, U = 0.f, Sr = 0.f, K = 0.f;
-        for (int j = tid; j < A; j += PL_BLOCK) {
-            const float tj = (ld(x + j) - m) * k, e = exp2f(tj);
-            S += e;
-            U += e * fmaxf(tj, -1e4f);                              // 0 log 0 = 0
-            if (EXACT) {
-                const float rj = (ld(y + j) - mr) * k;
-                Sr += exp2f(rj);
-                K += e > 0.f ? e * (tj - rj) : 0.f;
+        const double w = policy_weight(q, row, w_all, w_in);
+        T *const d = q.grad ? (T *)q.grad + (int64_t)row * q.grad_ld : nullptr;
+        const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
+        const int mis = policy_mis(x);
+        const bool same = EXACT && policy_mis(y) == mis, vec = d && policy_mis(d) == mis;
+        const bool live = w != 0.0;
+        PolicyRow r{};
+        float xa = 0.f;
+        if (live) { r = policy_inputs(q, row, w, tid == 0); xa = ld(x + r.a); }
+        auto piece = [&](const T *v, bool aligned, int j) {
+            return aligned && j >= 0 && j + V <= A ? *(const uint4 *)(v + j) : j < A ? policy_edge(v, j, A) : policy_none<T>();
+        };
+        float m[2] = {PL_LOWEST, PL_LOWEST}, s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (live)
+            for (int j0 = tid * V - mis; j0 < A; j0 += PL_PIECES * PL_STREAM * V) {
+                uint4 rx[PL_PIECES], ry[PL_PIECES];
+#pragma unroll
+                for (int c = 0; c < PL_PIECES; ++c) {
+                    const int j = j0 + c * PL_STREAM * V;
+                    rx[c] = piece(x, true, j);
+                    if (EXACT) ry[c] = piece(y, same, j);
+                }
+                float n[2] = {m[0], m[1]};
+#pragma unroll
+                for (int c = 0; c < PL_PIECES; ++c) P::max(rx[c], ry[c], n);
+                const float up = (m[0] - n[0]) * k, f = __builtin_amdgcn_exp2f(up);      // (m = n = lowest: 0 and 1)
+                if (EXACT) s[3] = s[0] > 0.f ? s[3] + s[0] * (up - (m[1] - n[1]) * k) : 0.f;
+                s[1] = __builtin_fmaf(s[0], fmaxf(up, PL_ZERO), s[1]);
+                s[0] *= f; s[1] *= f; s[3] *= f;
+                if (EXACT) s[2] *= __builtin_amdgcn_exp2f((m[1] - n[1]) * k);
+                m[0] = n[0]; m[1] = n[1];
+#pragma unroll
+                for (int c = 0; c < PL_PIECES; ++c) P::sums(rx[c], ry[c], m[0], m[1], k, s);
             }
+        float top[2] = {m[0], m[1]};
+        row_reduce<PL_STREAM>(top, OpMaxF(), s_max);
+        {
+            const float up = (m[0] - top[0]) * k, upr = (m[1] - top[1]) * k, f = __builtin_amdgcn_exp2f(up);
+            if (EXACT) s[3] = s[0] > 0.f ? s[3] + s[0] * (up - upr) : 0.f;
+            s[1] = __builtin_fmaf(s[0], fmaxf(up, PL_ZERO), s[1]) * f;
+            s[0] *= f; s[3] *= f;
+            if (EXACT) s[2] *= __builtin_amdgcn_exp2f(upr);
         }
-        PolicySums s;
-        s.S = (double)block_sum<PL_BLOCK>(S, red);
-        s.U = block_sum<PL_BLOCK>(U, red);
-        s.Sr = EXACT ? (double)block_sum<PL_BLOCK>(Sr, red) : 1.0;
-        s.K = EXACT ? block_sum<PL_BLOCK>(K, red) : 0.f;
-        if (s.S == 0.0) {                                           // no action is allowed
-            if (dst) for (int j = tid; j < A; j += PL_BLOCK) st(dst + j, 0.f);
-            if (tid == 0 && q.logp) q.logp[row] = -INFINITY;
-            continue;
-        }
-        PolicyRow r;
-        r.a = q.ids[row];
-        if (r.a < 0 || r.a >= A) { r.a = 0; if (tid == 0) atomicOr(q.flags, FLAG_BAD_ACTION); }
-        r.adv = q.adv ? q.adv[row] : 0.f;
-        r.old = q.old_logp ? q.old_logp[row] : 0.f;
-        r.ref = q.ref_logp ? q.ref_logp[row] : 0.f;
-        r.w = w;
-        const PolicyCoef c = policy_row(pc, r, s, ld(x + r.a) - m, q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        row_reduce<PL_STREAM>(s, OpAddF(), s_sum);
+        PolicyCoef c = policy_row(pc, r, PolicySums{s[0], s[2], s[1], s[3]}, xa - top[0], q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        const bool dead = !live || s[0] == 0.f;
+        if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
         if (tid == 0) {
             if (q.logp) q.logp[row] = c.logp;
             sum[0] += w * (double)c.pg;
@@ -175,15 +441,23 @@ k_policy_rows(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             sum[2] += w * (double)c.ent;
             sum[3] += w * (double)c.clipped;
         }
-        if (dst) {
-            __syncthreads();                                        // the gradient may replace the logits: x[a] has been read
-            for (int j = tid; j < A; j += PL_BLOCK) {
-                const float tj = (ld(x + j) - m) * k, e = exp2f(tj);
-                float f = c.alpha + c.gamma * fmaxf(tj, -1e4f);
-                if (EXACT) f += e > 0.f ? c.kappa * (tj - (ld(y + j) - mr) * k) : 0.f;
-                st(dst + j, e * f + (j == r.a ? c.hot : 0.f));
+        if (d)
+            for (int j0 = tid * V - mis; j0 < A; j0 += PL_PIECES * PL_STREAM * V) {
+                uint4 rx[PL_PIECES], ry[PL_PIECES];
+#pragma unroll
+                for (int i = 0; i < PL_PIECES; ++i) {
+                    const int j = j0 + i * PL_STREAM * V;
+                    rx[i] = dead ? policy_none<T>() : piece(x, true, j);
+                    if (EXACT) ry[i] = dead ? policy_none<T>() : piece(y, same, j);
+                }
+#pragma unroll
+                for (int i = 0; i < PL_PIECES; ++i) {
+                    const int j = j0 + i * PL_STREAM * V;
+                    float o[V];
+                    P::grad(rx[i], ry[i], top[0], top[1], k, c, r.a - j, o);
+                    if (j < A) policy_put(d, o, j, A, vec);
+                }
             }
-        }
     }
     if (tid == 0)
 #pragma unroll
@@ -216,6 +490,34 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
     }
 }
 
+// The row's kernel by its number of 16-byte pieces (one more than it has where it may begin between two boundaries).
+template <class T, bool EXACT>
+static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)
+{
+    const int64_t pieces = ((int64_t)q.A + 2 * Vec16<T>::N - 2) / Vec16<T>::N;
+    int grid = 0;
+    auto go = [&](auto kern, int block, int per) {
+        const int64_t n = ((int64_t)rows + per - 1) / per;
+        grid = (int)(n < PL_GRID ? n : PL_GRID);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
+    };
+#define HELD(L, C) go(k_policy_held<T, EXACT, L, C>, L > PL_BLOCK ? L : PL_BLOCK, (L > PL_BLOCK ? L : PL_BLOCK) / L)
+    if (pieces <= 8) HELD(8, 1);
+    else if (pieces <= 16) HELD(8, 2);
+    else if (pieces <= 32) HELD(8, 4);
+    else if (pieces <= 64) HELD(16, 4);
+    else if (pieces <= 128) HELD(32, 4);
+    else if (pieces <= 256) HELD(64, 4);
+    else if (pieces <= 1024) HELD(256, 4);
+    else if (pieces <= 2048) HELD(256, 8);
+    else if (pieces <= 4096) HELD(512, 8);
+    else if (pieces <= 8192) HELD(1024, 8);
+    else if (!EXACT && pieces <= 16384) HELD(1024, (EXACT ? 8 : 16));
+    else go(k_policy_stream<T, EXACT>, PL_STREAM, 1);
+#undef HELD
+    return grid;
+}
+
 // [partial sums][counts int32 B][weights double B]
 size_t policy_scratch_bytes(int B) { return (size_t)PL_GRID * 4 * sizeof(double) + (size_t)B * 16 + 64; }
 
@@ -230,10 +532,11 @@ void launch_policy_loss(const PolicyArgs &q, const PolicyCfg &g, void *scratch, 
         hipLaunchKernelGGL(k_policy_count, dim3(q.B), dim3(PL_BLOCK), 0, st, q.eff, q.T, n);
         hipLaunchKernelGGL(k_policy_weights, dim3(1), dim3(PL_BLOCK), 0, st, n, q.B, q.G, g.by_schedule, w);
     }
-    const int rows = q.B * q.G * q.T, grid = rows < PL_GRID ? rows : PL_GRID;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(grid), dim3(PL_BLOCK), 0, st, q, pc, w_all, w, partial); };
-    if (q.dtype == 1) { if (q.ref_logits) go(k_policy_rows<bf16_t, true>); else go(k_policy_rows<bf16_t, false>); }
-    else { if (q.ref_logits) go(k_policy_rows<float, true>); else go(k_policy_rows<float, false>); }
+    const int rows = q.B * q.G * q.T;
+    const int grid = q.dtype == 1 ? (q.ref_logits ? launch_rows<bf16_t, true>(q, pc, w_all, w, partial, rows, st)
+                                                  : launch_rows<bf16_t, false>(q, pc, w_all, w, partial, rows, st))
+                                  : (q.ref_logits ? launch_rows<float, true>(q, pc, w_all, w, partial, rows, st)
+                                                  : launch_rows<float, false>(q, pc, w_all, w, partial, rows, st));
     hipLaunchKernelGGL(k_policy_finish, dim3(1), dim3(PL_BLOCK), 0, st, partial, grid, pc, q.loss, q.stats);
 }
 

@@ -499,7 +499,8 @@ class Sol:
         """Clipped policy loss with KL term and entropy bonus of logits [B][G][T][A] (float32 or bfloat16, rows evenly spaced),
         forward and gradient. action_ids int32, adv / old_logp / ref_logp float32 [B][G][T] or None, ref_logits like logits or
         None, eff int32 [B][T] or None. Returns dict of device tensors: loss [1], stats [4] (policy term, KL, entropy, clipped
-        share), logp [B][G][T], grad like logits (grad_out if given, which may be logits itself; None if want_grad is false)."""
+        share), logp [B][G][T], grad [B][G][T][A] (grad_out if given, which may be logits itself; None if want_grad is false; of padded
+        logits, rows with up to seven unused elements between them)."""
         _need(logits.dim() == 4 and logits.dtype in _CODE, "logits: [B][G][T][A] of float32 or bfloat16 is needed")
         _need(logits.is_cuda and logits.device.index == torch.cuda.current_device(), "logits: not on the current device")
         _need(mean in MEANS, f"mean: one of {', '.join(MEANS)}")
@@ -515,7 +516,10 @@ class Sol:
             if t is not None:
                 _need(t.shape == logits.shape and t.dtype == logits.dtype and t.device == logits.device, f"{what}: not like logits")
         if want_grad and grad_out is None:
-            grad_out = torch.empty((B, G, T, A), dtype=logits.dtype, device=logits.device)
+            # rows of padded logits begin at other distances from 16 bytes than packed ones would: the gradient's as the logits' do
+            gap = (ld - A) % 8
+            grad_out = torch.empty((B, G, T, A + gap), dtype=logits.dtype, device=logits.device)
+            grad_out = grad_out[..., :A] if gap else grad_out
         loss = torch.zeros(1, dtype=torch.float32, device=logits.device) if B * G * T == 0 else logits.new_empty(1, dtype=torch.float32)
         stats, logp = loss.new_zeros(4) if B * G * T == 0 else loss.new_empty(4), loss.new_empty(steps)
         ws = loss.new_empty(self.L.sol_policy_workspace_bytes(B, G, T), dtype=torch.uint8)
