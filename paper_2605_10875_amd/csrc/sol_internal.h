@@ -248,10 +248,11 @@ struct PolicyArgs {
     float *loss, *stats, *logp;               // [1], [4] or NULL, [rows] or NULL
     int *flags;
     int dtype, B, G, T, A;                    // rows = B * G * T < 2^31
+    int pieces, by_schedule;                  // set by the launcher
 };
 struct PolicyCfg { double clip_low, clip_high, kl_coef, entropy_coef, temperature, scale; int by_schedule; };
 size_t policy_scratch_bytes(int B);
-void launch_policy_loss(const PolicyArgs &q, const PolicyCfg &g, void *scratch, hipStream_t st);
+void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStream_t st);
 
 // ---- gradient norm, clip and AdamW over many tensors (sol_update.hip) ----------------------------
 struct GradItem { void *g; int64_t n; int dtype; };

@@ -28,7 +28,29 @@ struct PolicyRow { int a; float adv, old, ref; double w; };
 struct PolicySums { float S, Sr, U, K; };
 struct PolicyCoef { float alpha, gamma, kappa, hot, logp, pg, kl, ent, clipped; };
 
-// w[b] = share of an effective step of input b in the mean (0: the input has none)
+// The share of an effective step of input b in the mean, 0 if the input has none. n: effective steps of the input, all: of all
+// inputs, or the inputs that have any (by_schedule), times the schedules.
+__device__ __forceinline__ double policy_share(int n, double all, int by_schedule)
+{
+    return n == 0 ? 0.0 : by_schedule ? 1.0 / ((double)n * all) : 1.0 / all;
+}
+
+// Few flags (PL_FEW of them, PL_INPUTS inputs at most): every workgroup counts them itself, which costs about a microsecond where
+// the two kernels below cost two launches.
+constexpr int PL_FEW = 4096, PL_INPUTS = 256;
+struct PolicyShares { int n[PL_INPUTS]; int all; };
+template <int BLOCK> __device__ __forceinline__ void policy_count(const PolicyArgs &q, PolicyShares &s)
+{
+    for (int b = threadIdx.x; b < q.B; b += BLOCK) s.n[b] = 0;
+    if (threadIdx.x == 0) s.all = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < q.B * q.T; i += BLOCK)
+        if (q.eff[i]) atomicAdd(&s.n[i / q.T], 1);
+    __syncthreads();
+    for (int b = threadIdx.x; b < q.B; b += BLOCK) atomicAdd(&s.all, q.by_schedule ? s.n[b] > 0 : s.n[b]);
+    __syncthreads();
+}
+
 __global__ void __launch_bounds__(PL_BLOCK)
 k_policy_count(const int32_t *__restrict__ eff, int T, int32_t *__restrict__ n)
 {
@@ -58,7 +80,7 @@ k_policy_weights(const int32_t *__restrict__ n, int B, int G, int by_schedule, d
     }
     const double all = (double)red[0] * (double)G;
     for (int b = threadIdx.x; b < B; b += PL_BLOCK)
-        w[b] = n[b] == 0 ? 0.0 : by_schedule ? 1.0 / ((double)n[b] * all) : 1.0 / all;
+        w[b] = policy_share(n[b], all, by_schedule);
 }
 
 // exp(u) - u - 1: by its series near 0, where the difference would keep a few bits only (|u| < 0.5: the first term left out
@@ -212,11 +234,12 @@ template <int LANES, int N, class Op> __device__ __forceinline__ void row_reduce
 }
 
 // A row's share of the loss, and its inputs but the logits
-__device__ __forceinline__ double policy_weight(const PolicyArgs &q, int row, double w_all, const double *w_in)
+__device__ __forceinline__ double policy_weight(const PolicyArgs &q, int row, double w_all, const double *w_in, const PolicyShares &few)
 {
     if (!q.eff) return w_all;
     const int b = row / (q.G * q.T), t = row % q.T;
-    return q.eff[(int64_t)b * q.T + t] ? w_in[b] : 0.0;
+    if (!q.eff[(int64_t)b * q.T + t]) return 0.0;
+    return w_in ? w_in[b] : policy_share(few.n[b], (double)few.all * (double)q.G, q.by_schedule);
 }
 __device__ __forceinline__ PolicyRow policy_inputs(const PolicyArgs &q, int row, double w, bool first)
 {
@@ -297,15 +320,17 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     constexpr int V = P::V, BLOCK = LANES > PL_BLOCK ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
     __shared__ float s_max[2][16], s_sum[4][16];
     __shared__ double s_part[BLOCK / 64][4];
+    __shared__ PolicyShares few;
+    if (q.eff && !w_in) policy_count<BLOCK>(q, few);
     const int tid = threadIdx.x, lane = tid % LANES, A = q.A;
     const float k = (float)pc.inv_temp * PL_LOG2E;
-    const int rows = q.B * q.G * q.T, used = (A + V - 1 + LANES * V - 1) / (LANES * V);     // pieces per lane, wherever the row begins
+    const int rows = q.B * q.G * q.T, used = (q.pieces + LANES - 1) / LANES;     // pieces per lane
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < rows; first += (int64_t)gridDim.x * ROWS) {
         const int64_t at = first + tid / LANES;
         const bool there = at < rows;                               // (the same for all lanes of a row, as live is)
         const int row = (int)(there ? at : rows - 1);
-        const double w = there ? policy_weight(q, row, w_all, w_in) : 0.0;
+        const double w = there ? policy_weight(q, row, w_all, w_in, few) : 0.0;
         const bool live = w != 0.0;
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
@@ -382,12 +407,14 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
     using P = PolicyPiece<T, EXACT>;
     constexpr int V = P::V;
     __shared__ float s_max[2][16], s_sum[4][16];
+    __shared__ PolicyShares few;
+    if (q.eff && !w_in) policy_count<PL_STREAM>(q, few);
     const int tid = threadIdx.x, A = q.A;
     const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-        const double w = policy_weight(q, row, w_all, w_in);
+        const double w = policy_weight(q, row, w_all, w_in, few);
         T *const d = q.grad ? (T *)q.grad + (int64_t)row * q.grad_ld : nullptr;
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
@@ -468,33 +495,33 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
 __global__ void __launch_bounds__(PL_BLOCK)
 k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, float *__restrict__ loss, float *__restrict__ stats)
 {
-    __shared__ double red[PL_BLOCK][4];
+    __shared__ double red[PL_BLOCK / 64][4];
     double v[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
     for (int i = threadIdx.x; i < n; i += PL_BLOCK)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += partial[4 * i + e];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) red[threadIdx.x][e] = v[e];
-    __syncthreads();
-    for (int o = PL_BLOCK / 2; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) red[threadIdx.x][e] += red[threadIdx.x + o][e];
-        __syncthreads();
+    for (int e = 0; e < 4; ++e) {
+        v[e] = lanes_sum_f64(v[e]);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6][e] = v[e];
     }
+    __syncthreads();
     if (threadIdx.x == 0) {
-        *loss = (float)(pc.scale * (red[0][0] + pc.kl * red[0][1] - pc.ent * red[0][2]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]);
+        *loss = (float)(pc.scale * (v[0] + pc.kl * v[1] - pc.ent * v[2]));
         if (stats)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) stats[e] = (float)red[0][e];
+            for (int e = 0; e < 4; ++e) stats[e] = (float)v[e];
     }
 }
 
-// The row's kernel by its number of 16-byte pieces (one more than it has where it may begin between two boundaries).
+// The row's kernel by its number of 16-byte pieces.
 template <class T, bool EXACT>
 static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)
 {
-    const int64_t pieces = ((int64_t)q.A + 2 * Vec16<T>::N - 2) / Vec16<T>::N;
+    const int64_t pieces = q.pieces;
     int grid = 0;
     auto go = [&](auto kern, int block, int per) {
         const int64_t n = ((int64_t)rows + per - 1) / per;
@@ -521,17 +548,24 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
 // [partial sums][counts int32 B][weights double B]
 size_t policy_scratch_bytes(int B) { return (size_t)PL_GRID * 4 * sizeof(double) + (size_t)B * 16 + 64; }
 
-void launch_policy_loss(const PolicyArgs &q, const PolicyCfg &g, void *scratch, hipStream_t st)
+void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStream_t st)
 {
+    // rows that may begin between two boundaries of 16 bytes touch one piece more
+    const size_t es = q.dtype == 1 ? 2 : 4;
+    const int64_t V = 16 / (int64_t)es;
+    const bool aligned = (uintptr_t)q.logits % 16 == 0 && (q.ld % V == 0 || (int64_t)q.B * q.G * q.T == 1);
+    q.pieces = (int)(((int64_t)q.A + (aligned ? 0 : V - 1) + V - 1) / V);
+    q.by_schedule = g.by_schedule;
     double *partial = (double *)scratch, *w = partial + 4 * PL_GRID;
     int32_t *n = (int32_t *)(w + q.B);
     const PolicyScalars pc{1.0 / g.temperature, log(1.0 - g.clip_low), log(1.0 + g.clip_high), 1.0 - g.clip_low, 1.0 + g.clip_high,
                            g.kl_coef, g.entropy_coef, g.scale};
     const double w_all = 1.0 / ((double)q.B * q.G * q.T);           // every step counts: both means are one
-    if (q.eff) {
+    const bool few = (int64_t)q.B * q.T <= PL_FEW && q.B <= PL_INPUTS;
+    if (q.eff && !few) {
         hipLaunchKernelGGL(k_policy_count, dim3(q.B), dim3(PL_BLOCK), 0, st, q.eff, q.T, n);
         hipLaunchKernelGGL(k_policy_weights, dim3(1), dim3(PL_BLOCK), 0, st, n, q.B, q.G, g.by_schedule, w);
-    }
+    } else w = nullptr;
     const int rows = q.B * q.G * q.T;
     const int grid = q.dtype == 1 ? (q.ref_logits ? launch_rows<bf16_t, true>(q, pc, w_all, w, partial, rows, st)
                                                   : launch_rows<bf16_t, false>(q, pc, w_all, w, partial, rows, st))

@@ -229,13 +229,13 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _on(t, dtype, shape, what):
-    """A contiguous tensor of the current device, or None."""
-    if t is not None:
-        _need(t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape),
-              f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the GPU is needed")
-        _need(t.device.index == torch.cuda.current_device(), f"{what}: not on the current device")
-    return t
+def _at(t, dtype, shape, here, what):
+    """Address of a contiguous tensor of device `here`, None if there is none."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the current device is needed")
+    return t.data_ptr()
 
 
 def _row_step(t, what):
@@ -501,37 +501,44 @@ class Sol:
         None, eff int32 [B][T] or None. Returns dict of device tensors: loss [1], stats [4] (policy term, KL, entropy, clipped
         share), logp [B][G][T], grad [B][G][T][A] (grad_out if given, which may be logits itself; None if want_grad is false; of padded
         logits, rows with up to seven unused elements between them)."""
-        _need(logits.dim() == 4 and logits.dtype in _CODE, "logits: [B][G][T][A] of float32 or bfloat16 is needed")
-        _need(logits.is_cuda and logits.device.index == torch.cuda.current_device(), "logits: not on the current device")
-        _need(mean in MEANS, f"mean: one of {', '.join(MEANS)}")
-        B, G, T, A = logits.shape
-        ld = _row_step(logits, "logits")
-        steps = (B, G, T)
-        for t, what in ((adv, "adv"), (old_logp, "old_logp"), (ref_logp, "ref_logp")):
-            _on(t, torch.float32, steps, what)
+        here, dtype, shape = torch.cuda.current_device(), logits.dtype, logits.shape
+        code = _CODE.get(dtype)
+        _need(code is not None and len(shape) == 4 and logits.get_device() == here,
+              "logits: [B][G][T][A] of float32 or bfloat16 on the current device is needed")
+        _need(mean in MEANS, "mean: 'steps' or 'schedules'")
         _need(action_ids is not None, "action_ids are needed")
-        _on(action_ids, torch.int32, steps, "action_ids")
-        _on(eff, torch.int32, (B, T), "eff")
+        B, G, T, A = shape
+        steps = shape[:3]
+        ids = _at(action_ids, torch.int32, steps, here, "action_ids")
+        adv, old_logp, ref_logp = (_at(t, torch.float32, steps, here, what)
+                                   for t, what in ((adv, "adv"), (old_logp, "old_logp"), (ref_logp, "ref_logp")))
+        eff = _at(eff, torch.int32, (B, T), here, "eff")
         for t, what in ((ref_logits, "ref_logits"), (grad_out, "grad_out")):
-            if t is not None:
-                _need(t.shape == logits.shape and t.dtype == logits.dtype and t.device == logits.device, f"{what}: not like logits")
-        if want_grad and grad_out is None:
+            _need(t is None or (t.shape == shape and t.dtype == dtype and t.get_device() == here), f"{what}: not like logits")
+        ld = _row_step(logits, "logits")
+        if not want_grad:
+            grad_out = None
+        elif grad_out is None:
             # rows of padded logits begin at other distances from 16 bytes than packed ones would: the gradient's as the logits' do
             gap = (ld - A) % 8
-            grad_out = torch.empty((B, G, T, A + gap), dtype=logits.dtype, device=logits.device)
-            grad_out = grad_out[..., :A] if gap else grad_out
-        loss = torch.zeros(1, dtype=torch.float32, device=logits.device) if B * G * T == 0 else logits.new_empty(1, dtype=torch.float32)
-        stats, logp = loss.new_zeros(4) if B * G * T == 0 else loss.new_empty(4), loss.new_empty(steps)
-        ws = loss.new_empty(self.L.sol_policy_workspace_bytes(B, G, T), dtype=torch.uint8)
+            grad_out = logits.new_empty((B, G, T, A + gap))
+            if gap:
+                grad_out = grad_out[..., :A]
+        # one allocation: loss, stats, log-probabilities; one for the workspace
+        n = B * G * T
+        out = torch.empty(8 + n, dtype=torch.float32, device="cuda") if n else torch.zeros(8, dtype=torch.float32, device="cuda")
+        loss, stats, logp = out[:1], out[4:8], out[8:].view(steps)
+        need = self.L.sol_policy_workspace_bytes(B, G, T)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
         cfg = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean])
-        grad = grad_out if want_grad else None
+        at = out.data_ptr()
         self._check(self.L.sol_policy_loss(
-            self.handle, _ptr(logits), _CODE[logits.dtype], ld, _ptr(action_ids), _ptr(adv), _ptr(old_logp), _ptr(ref_logp),
-            _ptr(ref_logits), _row_step(ref_logits, "ref_logits") if ref_logits is not None else 0, _ptr(eff), C.byref(cfg), B, G, T, A,
-            _ptr(loss), _ptr(stats), _ptr(logp), _ptr(grad), _row_step(grad, "grad_out") if grad is not None else 0, _ptr(ws),
-            ws.numel(), _stream(stream)))
-        _used_on(stream, ws, loss, stats, logp, grad)
-        return {"loss": loss, "stats": stats, "logp": logp, "grad": grad}
+            self.handle, logits.data_ptr(), code, ld, ids, adv, old_logp, ref_logp, None if ref_logits is None else ref_logits.data_ptr(),
+            0 if ref_logits is None else _row_step(ref_logits, "ref_logits"), eff, C.byref(cfg), B, G, T, A, at, at + 16, at + 32,
+            None if grad_out is None else grad_out.data_ptr(), 0 if grad_out is None else _row_step(grad_out, "grad_out"), ws.data_ptr(), need,
+            _stream(stream)))
+        _used_on(stream, ws, out, grad_out)
+        return {"loss": loss, "stats": stats, "logp": logp, "grad": grad_out}
 
     def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
         """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
@@ -567,13 +574,11 @@ class Sol:
             flat += (p.data_ptr(), exp_avg[i].data_ptr(), exp_avg_sq[i].data_ptr(), g.data_ptr(), 0 if c is None else c.data_ptr(), size,
                      _CODE[g.dtype])
         arr = (C.c_int64 * len(flat))(*flat)
-        by_tensor = isinstance(lr, torch.Tensor)
-        for t, dtype, what in ((step, torch.int32, "step"), (coef, torch.float32, "coef"), (lr if by_tensor else None, torch.float32, "lr")):
-            _need(t is None or t.numel() == 1, f"{what}: one element is needed")
-            _on(t, dtype, () if t is None else t.shape, what)
+        here, by_tensor = torch.cuda.current_device(), isinstance(lr, torch.Tensor)
+        step, coef, rate = (_at(t, dtype, (1,), here, what) for t, dtype, what in
+                            ((step, torch.int32, "step"), (coef, torch.float32, "coef"), (lr if by_tensor else None, torch.float32, "lr")))
         cfg = AdamwCfg(0.0 if by_tensor else lr, betas[0], betas[1], eps, weight_decay)
-        self._check(self.L.sol_adamw_step(self.handle, arr, n, C.byref(cfg), _ptr(step), _ptr(lr) if by_tensor else None, _ptr(coef),
-                                          _stream(stream)))
+        self._check(self.L.sol_adamw_step(self.handle, arr, n, C.byref(cfg), step, rate, coef, _stream(stream)))
 
     def schedule_loglik(self, layers, head, tokens, targets, action_ids, nll_out=None, workspace=None, stream=None):
         """tokens/targets int32 [B][T]; action_ids int32 [B][G][T]. Returns nll float32 [B][G][T] (nats)."""
