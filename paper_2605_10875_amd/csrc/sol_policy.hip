@@ -4,12 +4,13 @@
 //   pg = -min(rho A, clip(rho, 1 - lo, 1 + hi) A),  H = -sum p_j logp_j
 //   KL = exp(u) - u - 1 with u = ref - logp_a (estimate), or sum p_j (logp_j - logq_j) (exact, from reference logits y_j)
 //   loss = scale * sum w (pg + beta KL - c H), w the row's share in the mean
-// With the row's maximum m, e_j = 2^(t_j), t_j = (x_j - m) log2(e) / temperature, S = sum e_j, U = sum e_j t_j and, with a
-// reference, t'_j, S' likewise and K = sum e_j (t_j - t'_j):
+// With the row's maximum m, t_j = (x_j - m) log2(e) / temperature, e_j = 2^(t_j), S = sum e_j,
+// U = sum e_j t_j and, with a reference, t'_j, S' likewise and K = sum e_j (t_j - t'_j):
 //   H = log S - ln2 U / S,  KL = ln2 K / S - (log S - log S')
 //   d loss / d x_j = p_j (alpha + gamma t_j + kappa (t_j - t'_j)) + [j = a] w' G
 // where w' = w scale / temperature, G = d(pg + beta KL) / d logp_a, gamma = w' c ln2, kappa = w' beta ln2 and
 // alpha = -w' (G + c ln2 U / S + beta ln2 K / S): the row needs its sums once, then every element's gradient by itself.
+// Where e_j is 0 (x_j = -inf above all) its products are 0 whatever the other factor is: times().
 #include "sol_internal.h"
 
 namespace sol {
@@ -19,13 +20,12 @@ constexpr int PL_GRID = 2048;                                       // workgroup
 constexpr float PL_LOG2E = 1.44269504088896341f;
 constexpr double PL_LN2 = 0.693147180559945309;
 constexpr float PL_LOWEST = -3.402823466e38f;                       // below every finite logit's maximum: no NaN from -inf - -inf
-constexpr float PL_ZERO = -1e4f;                                    // 2^t is zero from here on: bounds t where t times zero is taken
 
-struct PolicyScalars { double inv_temp, log_lo, log_hi, lo, hi, kl, ent, scale; };
+struct PolicyScalars { double inv_temp, log_lo, log_hi, factor, kl, ent, scale; float lo, hi; };      // factor: scale / temperature
 
 // what a row needs besides its sums
 struct PolicyRow { int a; float adv, old, ref; double w; };
-struct PolicySums { float S, Sr, U, K; };
+struct PolicySums { float S, Sr, U, K, xa; };                       // xa: the taken action's logit
 struct PolicyCoef { float alpha, gamma, kappa, hot, logp, pg, kl, ent, clipped; };
 
 // The share of an effective step of input b in the mean, 0 if the input has none. n: effective steps of the input, all: of all
@@ -44,8 +44,18 @@ template <int BLOCK> __device__ __forceinline__ void policy_count(const PolicyAr
     for (int b = threadIdx.x; b < q.B; b += BLOCK) s.n[b] = 0;
     if (threadIdx.x == 0) s.all = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < q.B * q.T; i += BLOCK)
-        if (q.eff[i]) atomicAdd(&s.n[i / q.T], 1);
+    // 64 flags at a time: the first lane of each input among them adds what its part of the wave's ballot counts
+    for (int at = threadIdx.x & ~63; at < q.B * q.T; at += BLOCK) {
+        const int lane = threadIdx.x & 63, i = at + lane;
+        const bool in = i < q.B * q.T;
+        const unsigned long long set = __ballot(in && q.eff[in ? i : 0] != 0);
+        const int b = i / q.T, t = i - b * q.T;
+        if (in && (lane == 0 || t == 0)) {
+            const int len = q.T - t < 64 - lane ? q.T - t : 64 - lane;
+            const int c = __popcll((set >> lane) & (len == 64 ? ~0ull : (1ull << len) - 1));
+            if (c) atomicAdd(&s.n[b], c);
+        }
+    }
     __syncthreads();
     for (int b = threadIdx.x; b < q.B; b += BLOCK) atomicAdd(&s.all, q.by_schedule ? s.n[b] > 0 : s.n[b]);
     __syncthreads();
@@ -122,18 +132,35 @@ __device__ __forceinline__ double policy_log(double x)
     return __builtin_fma((double)k, PL_LN2, s * p);
 }
 
-// The row's loss terms and the coefficients of its gradient from its sums. xa: the taken action's logit minus the maximum.
-// The ratio's bounds are tested on its logarithm in 64 bits: a gradient is not continuous there.
-__device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const PolicyRow &r, const PolicySums &s, float xa,
+// t of a logit f. As one fma, c = -m k rounded: every t of the row is then off by the same fma(m, k, c), which cancels in p, H and KL and
+// which policy_row takes out of the log-probability. That holds while the offset is small, |m k| <= PL_FAR (offset below 1/4; c is
+// bounded by it, so that it stays finite); rows beyond it are centred first (policy_centred), or take the difference itself (SUB).
+constexpr float PL_FAR = 4194304.f;
+struct PolicyScale { float k, c; };
+template <bool SUB> __device__ __forceinline__ PolicyScale policy_scale(float m, float k)
+{
+    return PolicyScale{k, SUB ? m : -fminf(fmaxf(m * k, -PL_FAR), PL_FAR)};
+}
+template <bool SUB> __device__ __forceinline__ float policy_t(float f, PolicyScale z)
+{
+    return SUB ? (f - z.c) * z.k : __builtin_fmaf(f, z.k, z.c);
+}
+// a b, 0 where a or b is 0 (also against infinities and NaN): v_mul_legacy_f32, which has no builtin of clang
+extern "C" __device__ float sol_mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float times(float a, float b) { return sol_mul_legacy(a, b); }
+
+// The row's loss terms and the coefficients of its gradient from its sums. The ratio's bounds are tested on its logarithm in 64 bits: a
+// gradient is not continuous there. m: the row's maximum, off: its t.
+__device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const PolicyRow &r, const PolicySums &s, float m, float off,
                                                  bool has_old, bool has_ref, bool exact_kl)
 {
     PolicyCoef c;
-    const double logS = policy_log((double)s.S), logp = (double)xa * pc.inv_temp - logS;
+    const double logS = policy_log((double)s.S), logp = ((double)s.xa - (double)m) * pc.inv_temp + (double)off * PL_LN2 - logS;
     const double d = has_old ? logp - (double)r.old : 0.0;
     const float A = r.adv, rho = expf((float)d);
     const bool clipped = (A > 0.f && d > pc.log_hi) || (A < 0.f && d < pc.log_lo);
     c.logp = (float)logp;
-    c.pg = clipped ? -(A > 0.f ? (float)pc.hi : (float)pc.lo) * A : -rho * A;
+    c.pg = clipped ? -(A > 0.f ? pc.hi : pc.lo) * A : -rho * A;
     float G = clipped ? 0.f : -rho * A;
     const float beta = (float)pc.kl, ln2 = (float)PL_LN2, inv = 1.f / s.S, u_mean = ln2 * s.U * inv;
     c.ent = (float)(logS - (double)u_mean);
@@ -148,7 +175,7 @@ __device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const 
         G -= beta * (u + c.kl);                                     // 1 - exp(u)
     }
     c.clipped = clipped ? 1.f : 0.f;
-    const float w = (float)(r.w * pc.scale * pc.inv_temp), ent = (float)pc.ent;
+    const float w = (float)(r.w * pc.factor), ent = (float)pc.ent;
     c.hot = w * G;
     c.alpha = -w * (G + ent * u_mean + (exact_kl ? beta * k_mean : 0.f)) * inv;
     c.gamma = w * ent * ln2 * inv;
@@ -233,6 +260,21 @@ template <int LANES, int N, class Op> __device__ __forceinline__ void row_reduce
     }
 }
 
+// the values that a row without (with) a reference has: 1 of 2 maxima; S, U and the logit of 5 sums
+template <int LANES, bool EXACT, int N, class Op> __device__ __forceinline__ void reduce_some(float (&v)[N], Op op, float (*slot)[16])
+{
+    if constexpr (EXACT) row_reduce<LANES>(v, op, slot);
+    else if constexpr (N == 2) {
+        float u[1] = {v[0]};
+        row_reduce<LANES>(u, op, slot);
+        v[0] = u[0];
+    } else {
+        float u[3] = {v[0], v[1], v[4]};
+        row_reduce<LANES>(u, op, slot);
+        v[0] = u[0]; v[1] = u[1]; v[4] = u[2];
+    }
+}
+
 // A row's share of the loss, and its inputs but the logits
 __device__ __forceinline__ double policy_weight(const PolicyArgs &q, int row, double w_all, const double *w_in, const PolicyShares &few)
 {
@@ -240,6 +282,13 @@ __device__ __forceinline__ double policy_weight(const PolicyArgs &q, int row, do
     const int b = row / (q.G * q.T), t = row % q.T;
     if (!q.eff[(int64_t)b * q.T + t]) return 0.0;
     return w_in ? w_in[b] : policy_share(few.n[b], (double)few.all * (double)q.G, q.by_schedule);
+}
+// the same for all lanes of a wave
+__device__ __forceinline__ double uniform(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b), hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ PolicyRow policy_inputs(const PolicyArgs &q, int row, double w, bool first)
 {
@@ -253,14 +302,18 @@ __device__ __forceinline__ PolicyRow policy_inputs(const PolicyArgs &q, int row,
     return r;
 }
 
-template <class T, bool EXACT> struct PolicyPiece {
+template <class T, bool EXACT, bool SUB> struct PolicyPiece {
     static constexpr int V = Vec16<T>::N;
-    static __device__ __forceinline__ void max(uint4 rx, uint4 ry, float (&m)[2])
+    // xa: the logit `at` elements behind the piece's first, if it is among them
+    static __device__ __forceinline__ void max(uint4 rx, uint4 ry, int at, float (&m)[2], float &xa)
     {
         float f[V];
         policy_unpack<T>(rx, f);
 #pragma unroll
         for (int i = 0; i < V; ++i) m[0] = fmaxf(m[0], f[i]);
+        if ((unsigned)at < (unsigned)V)
+#pragma unroll
+            for (int i = 0; i < V; ++i) xa = i == at ? f[i] : xa;
         if (EXACT) {
             policy_unpack<T>(ry, f);
 #pragma unroll
@@ -268,38 +321,71 @@ template <class T, bool EXACT> struct PolicyPiece {
         }
     }
     // s: S, U, S', K
-    static __device__ __forceinline__ void sums(uint4 rx, uint4 ry, float m, float mr, float k, float (&s)[4])
+    static __device__ __forceinline__ void sums(uint4 rx, uint4 ry, PolicyScale z, PolicyScale zr, float (&s)[5])
     {
         float f[V], g[V];
         policy_unpack<T>(rx, f);
         if (EXACT) policy_unpack<T>(ry, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float t = (f[i] - m) * k, e = __builtin_amdgcn_exp2f(t);
+            const float t = policy_t<SUB>(f[i], z), e = __builtin_amdgcn_exp2f(t);
             s[0] += e;
-            s[1] = __builtin_fmaf(e, fmaxf(t, PL_ZERO), s[1]);
+            s[1] += times(e, t);
             if (EXACT) {
-                const float r = (g[i] - mr) * k;
+                const float r = policy_t<SUB>(g[i], zr);
                 s[2] += __builtin_amdgcn_exp2f(r);
-                s[3] += e > 0.f ? e * (t - r) : 0.f;
+                s[3] += times(e, t - r);
             }
         }
     }
-    static __device__ __forceinline__ void grad(uint4 rx, uint4 ry, float m, float mr, float k, const PolicyCoef &c, int at, float (&o)[V])
+    static __device__ __forceinline__ void grad(uint4 rx, uint4 ry, PolicyScale z, PolicyScale zr, const PolicyCoef &c, int at, float (&o)[V])
     {
         float f[V], g[V];
         policy_unpack<T>(rx, f);
         if (EXACT) policy_unpack<T>(ry, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float t = (f[i] - m) * k, e = __builtin_amdgcn_exp2f(t);
-            float h = __builtin_fmaf(c.gamma, fmaxf(t, PL_ZERO), c.alpha);
-            if (EXACT) h += e > 0.f ? c.kappa * (t - (g[i] - mr) * k) : 0.f;
-            o[i] = e * h;
+            const float t = policy_t<SUB>(f[i], z), e = __builtin_amdgcn_exp2f(t);
+            float h = __builtin_fmaf(c.gamma, t, c.alpha);
+            if (EXACT) h = __builtin_fmaf(c.kappa, t - policy_t<SUB>(g[i], zr), h);
+            o[i] = times(e, h);
         }
-        if ((unsigned)at < (unsigned)V)                             // the action taken is among them
+        if ((unsigned)at < (unsigned)V)
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] += i == at ? c.hot : 0.f;
+    }
+};
+
+// Rows beyond PL_FAR: logits minus the maximum. bf16 logits of that size lie 2^13 / k apart at least, so that rounding a difference
+// that is not 0 back to 8 bits leaves 2^t = 0.
+__device__ __forceinline__ bool policy_is_far(float m, float k) { return !(fabsf(m * k) <= PL_FAR); }
+template <class T> __device__ __forceinline__ uint4 policy_centred(uint4 raw, float m)
+{
+    constexpr int V = Vec16<T>::N;
+    float f[V];
+    policy_unpack<T>(raw, f);
+    if (sizeof(T) == 4) return make_uint4(__float_as_uint(f[0] - m), __float_as_uint(f[1] - m), __float_as_uint(f[2] - m), __float_as_uint(f[3] - m));
+    return make_uint4(pack_bf16x2(f[0] - m, f[1] - m), pack_bf16x2(f[2] - m, f[3] - m), pack_bf16x2(f[4 % V] - m, f[5 % V] - m),
+                      pack_bf16x2(f[6 % V] - m, f[7 % V] - m));
+}
+
+// Sums of a lane relative to a running maximum: turn() makes them relative to a larger one.
+template <bool EXACT, bool SUB> struct PolicyRunning {
+    float m[2] = {PL_LOWEST, PL_LOWEST}, s[5] = {0.f, 0.f, 0.f, 0.f, 0.f}, k;
+    PolicyScale z, zr;
+    __device__ __forceinline__ explicit PolicyRunning(float scale) : k(scale) { z = zr = policy_scale<SUB>(m[0], k); }
+    __device__ __forceinline__ void turn(const float (&n)[2])
+    {
+        const PolicyScale y = policy_scale<SUB>(n[0], k), yr = EXACT ? policy_scale<SUB>(n[1], k) : y;
+        if (s[0] > 0.f) {                                           // t' = t + up
+            const float up = policy_t<SUB>(m[0], y) - policy_t<SUB>(m[0], z), f = __builtin_amdgcn_exp2f(up);
+            if (EXACT) s[3] = times(f, __builtin_fmaf(s[0], up - (policy_t<SUB>(m[1], yr) - policy_t<SUB>(m[1], zr)), s[3]));
+            s[1] = times(f, __builtin_fmaf(s[0], up, s[1]));
+            s[0] = times(f, s[0]);
+        }
+        if (EXACT && s[2] > 0.f) s[2] *= __builtin_amdgcn_exp2f(policy_t<SUB>(m[1], yr) - policy_t<SUB>(m[1], zr));
+        z = y; zr = yr;
+        m[0] = n[0]; m[1] = n[1];
     }
 };
 
@@ -313,12 +399,12 @@ __device__ __forceinline__ double lanes_sum_f64(double v)
 // A row in the registers of LANES lanes, CH pieces of 16 bytes per lane: it is read once, all lanes wait for nothing but the row's
 // maximum and its sums. LANES <= 64: several rows per wave, side by side, no LDS.
 template <class T, bool EXACT, int LANES, int CH>
-__global__ void __launch_bounds__(LANES > PL_BLOCK ? LANES : PL_BLOCK)
+__global__ void __launch_bounds__(LANES > PL_BLOCK ? LANES : PL_BLOCK, LANES == 512 ? 4 : 1)
 k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
 {
-    using P = PolicyPiece<T, EXACT>;
+    using P = PolicyPiece<T, EXACT, false>;
     constexpr int V = P::V, BLOCK = LANES > PL_BLOCK ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
-    __shared__ float s_max[2][16], s_sum[4][16];
+    __shared__ float s_max[2][16], s_sum[5][16];
     __shared__ double s_part[BLOCK / 64][4];
     __shared__ PolicyShares few;
     if (q.eff && !w_in) policy_count<BLOCK>(q, few);
@@ -345,24 +431,31 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             if (EXACT) ry[EXACT ? (int)c : 0] = whole && same ? *(const uint4 *)(y + j) : policy_none<T>();
         });
         PolicyRow r{};
-        float xa = 0.f;
-        if (live) {
-            r = policy_inputs(q, row, w, lane == 0);
-            xa = ld(x + r.a);
-        }
+        if (live) r = policy_inputs(q, row, w, lane == 0);
         pieces([&](auto c, int j) {
             const bool part = live && j < A, cut = j < 0 || j + V > A;
             if (part && cut) rx[c] = policy_edge(x, j, A);
             if (EXACT && part && (cut || !same)) ry[EXACT ? (int)c : 0] = policy_edge(y, j, A);
         });
-        float m[2] = {PL_LOWEST, PL_LOWEST}, s[4] = {0.f, 0.f, 0.f, 0.f};
-        pieces([&](auto c, int) { P::max(rx[c], ry[EXACT ? (int)c : 0], m); });
-        if (EXACT) row_reduce<LANES>(m, OpMaxF(), s_max);
-        else { float one[1] = {m[0]}; row_reduce<LANES>(one, OpMaxF(), s_max); m[0] = one[0]; }
-        pieces([&](auto c, int) { P::sums(rx[c], ry[EXACT ? (int)c : 0], m[0], m[1], k, s); });
-        if (EXACT) row_reduce<LANES>(s, OpAddF(), s_sum);
-        else { float two[2] = {s[0], s[1]}; row_reduce<LANES>(two, OpAddF(), s_sum); s[0] = two[0]; s[1] = two[1]; }
-        PolicyCoef c = policy_row(pc, r, PolicySums{s[0], s[2], s[1], s[3]}, xa - m[0], q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        float m[2] = {PL_LOWEST, PL_LOWEST}, s[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+        pieces([&](auto c, int j) { P::max(rx[c], ry[EXACT ? (int)c : 0], r.a - j, m, s[4]); });
+        reduce_some<LANES, EXACT, 2>(m, OpMaxF(), s_max);
+        const float top = m[0];
+        const bool far = policy_is_far(m[0], k), far_ref = EXACT && policy_is_far(m[1], k);
+        if (__any(far || far_ref)) {
+            pieces([&](auto c, int) {
+                if (far) rx[c] = policy_centred<T>(rx[c], m[0]);
+                if (EXACT && far_ref) ry[EXACT ? (int)c : 0] = policy_centred<T>(ry[EXACT ? (int)c : 0], m[1]);
+            });
+            m[0] = far ? 0.f : m[0];
+            m[1] = far_ref ? 0.f : m[1];
+        }
+        PolicyScale z = policy_scale<false>(m[0], k), zr = EXACT ? policy_scale<false>(m[1], k) : z;
+        pieces([&](auto c, int) { P::sums(rx[c], ry[EXACT ? (int)c : 0], z, zr, s); });
+        reduce_some<LANES, EXACT, 5>(s, OpAddF(), s_sum);
+        PolicyCoef c = policy_row(pc, r, PolicySums{s[0], s[2], s[1], s[3], s[4]}, top, policy_t<false>(m[0], z), q.old_logp != nullptr,
+                                  q.ref_logp != nullptr, EXACT);
+        if (s[0] != s[0]) z.c = NAN;                                // (no distribution: no element's 2^t is 0)
         const bool dead = !live || s[0] == 0.f;                     // not an effective step, or no action allowed
         if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
         if (there && lane == 0) {
@@ -377,7 +470,7 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             const bool vec = policy_mis(d) == mis;
             pieces([&](auto i, int j) {
                 float o[V];
-                P::grad(rx[i], ry[EXACT ? (int)i : 0], m[0], m[1], k, c, r.a - j, o);
+                P::grad(rx[i], ry[EXACT ? (int)i : 0], z, zr, c, r.a - j, o);
                 if (j < A) policy_put(d, o, j, A, vec);
             });
         }
@@ -397,69 +490,169 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     }
 }
 
+// A row in the registers of one workgroup per CU, CH pieces per lane of each of its 1024: too large for a second workgroup that would
+// work while this one waits for memory, so each piece of the next row is requested as soon as this row's gradient has left its
+// registers, and the sums start with the pieces that are there. Workgroups take rows in turn.
+template <class T, bool EXACT, int BLOCK, int CH>
+__global__ void __launch_bounds__(BLOCK, 4)
+k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
+{
+    using P = PolicyPiece<T, EXACT, false>;
+    constexpr int V = P::V, GROUP = EXACT ? 1 : 2;                  // pieces between two looks at the maximum
+    __shared__ float s_max[2][16], s_sum[5][16];
+    __shared__ PolicyShares few;
+    if (q.eff && !w_in) policy_count<BLOCK>(q, few);
+    const int tid = threadIdx.x, A = q.A;
+    const float k = (float)pc.inv_temp * PL_LOG2E;
+    const int rows = q.B * q.G * q.T, used = (q.pieces + BLOCK - 1) / BLOCK;
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    uint4 rx[CH], ry[EXACT ? CH : 1];
+    const T *x = nullptr, *y = nullptr;                             // the row that is being loaded
+    int mis = 0;
+    bool same = false, live = false;
+    double w = 0.0;
+    auto start = [&](int64_t row) {
+        w = row < rows ? uniform(policy_weight(q, (int)row, w_all, w_in, few)) : 0.0;
+        live = w != 0.0;
+        if (!live) return;
+        x = (const T *)q.logits + row * q.ld;
+        y = EXACT ? (const T *)q.ref_logits + row * q.ref_ld : nullptr;
+        mis = policy_mis(x);
+        same = EXACT && policy_mis(y) == mis;
+    };
+    auto request = [&](auto i) {
+        const int j = ((int)i * BLOCK + tid) * V - mis;
+        const bool whole = j >= 0 && j + V <= A;
+        rx[i] = !live || j >= A ? policy_none<T>() : whole ? *(const uint4 *)(x + j) : policy_edge(x, j, A);
+        if (EXACT) ry[EXACT ? (int)i : 0] = !live || j >= A ? policy_none<T>() : whole && same ? *(const uint4 *)(y + j) : policy_edge(y, j, A);
+    };
+    start(blockIdx.x);
+    static_for<CH>([&](auto i) { if (i < used) request(i); });
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const double w_row = w;
+        const bool live_row = live;
+        const int mis_row = mis;
+        PolicyRow r{};
+        if (live_row) r = policy_inputs(q, (int)row, w_row, tid == 0);
+        PolicyRunning<EXACT, false> u(k);
+        float xa = 0.f, top;
+        for (bool centred = false;; centred = true) {               // twice where the maximum is far from 0
+            static_for<(CH + GROUP - 1) / GROUP>([&](auto g) {
+                if (g * GROUP < used) {
+                    float n[2] = {u.m[0], u.m[1]};
+                    static_for<GROUP>([&](auto e) {
+                        constexpr int i = decltype(g)::value * GROUP + decltype(e)::value;
+                        if (i < used) P::max(rx[i], ry[EXACT ? i : 0], centred ? -1 : r.a - ((i * BLOCK + tid) * V - mis_row), n, xa);
+                    });
+                    u.turn(n);
+                    static_for<GROUP>([&](auto e) {
+                        constexpr int i = decltype(g)::value * GROUP + decltype(e)::value;
+                        if (i < used) P::sums(rx[i], ry[EXACT ? i : 0], u.z, u.zr, u.s);
+                    });
+                }
+                __builtin_amdgcn_sched_barrier(0);                  // (all groups' elements at once do not fit the registers)
+            });
+            float n[2] = {u.m[0], u.m[1]};
+            reduce_some<BLOCK, EXACT, 2>(n, OpMaxF(), s_max);
+            if (!centred) top = n[0];
+            const bool far = policy_is_far(n[0], k), far_ref = EXACT && policy_is_far(n[1], k);
+            if (centred || !(far || far_ref)) { u.turn(n); break; }
+            static_for<CH>([&](auto i) {
+                if (i < used) {
+                    if (far) rx[i] = policy_centred<T>(rx[i], n[0]);
+                    if (EXACT && far_ref) ry[EXACT ? (int)i : 0] = policy_centred<T>(ry[EXACT ? (int)i : 0], n[1]);
+                }
+            });
+            u = PolicyRunning<EXACT, false>(k);
+            __syncthreads();                                        // (s_max is written again without another use of s_sum between)
+        }
+        u.s[4] = xa;
+        reduce_some<BLOCK, EXACT, 5>(u.s, OpAddF(), s_sum);
+        PolicyCoef c = policy_row(pc, r, PolicySums{u.s[0], u.s[2], u.s[1], u.s[3], u.s[4]}, top, policy_t<false>(u.m[0], u.z),
+                                  q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        if (u.s[0] != u.s[0]) u.z.c = NAN;
+        if (!live_row || u.s[0] == 0.f) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live_row ? -INFINITY : 0.f; }
+        if (tid == 0) {
+            if (q.logp) q.logp[row] = c.logp;
+            sum[0] += w_row * (double)c.pg;
+            sum[1] += w_row * (double)c.kl;
+            sum[2] += w_row * (double)c.ent;
+            sum[3] += w_row * (double)c.clipped;
+        }
+        T *const d = q.grad ? (T *)q.grad + row * q.grad_ld : nullptr;
+        const bool vec = policy_mis(d) == mis_row;
+        start(row + gridDim.x);
+        static_for<CH>([&](auto i) {
+            if (i < used) {
+                if (d) {
+                    const int j = ((int)i * BLOCK + tid) * V - mis_row;
+                    float o[V];
+                    P::grad(rx[i], ry[EXACT ? (int)i : 0], u.z, u.zr, c, r.a - j, o);
+                    if (j < A) policy_put(d, o, j, A, vec);
+                }
+                request(i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    }
+    if (tid == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) partial[4 * (int64_t)blockIdx.x + i] = sum[i];
+}
+
 // A row that does not fit: one workgroup, two sweeps. The first keeps a running maximum per lane, its sums scaled anew where the
-// maximum of the next PIECES pieces is larger; the second reads the row again, from the caches where the rows in flight fit them.
-constexpr int PL_STREAM = 512, PL_PIECES = 4;
-template <class T, bool EXACT>
-__global__ void __launch_bounds__(PL_STREAM)
+// maximum of the next CH pieces is larger; the second reads the row again, from the caches where the rows in flight fit them.
+template <class T, bool EXACT, int BLOCK, int CH>
+__global__ void __launch_bounds__(BLOCK)
 k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
 {
-    using P = PolicyPiece<T, EXACT>;
+    using P = PolicyPiece<T, EXACT, true>;
     constexpr int V = P::V;
-    __shared__ float s_max[2][16], s_sum[4][16];
+    __shared__ float s_max[2][16], s_sum[5][16];
     __shared__ PolicyShares few;
-    if (q.eff && !w_in) policy_count<PL_STREAM>(q, few);
+    if (q.eff && !w_in) policy_count<BLOCK>(q, few);
     const int tid = threadIdx.x, A = q.A;
     const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-        const double w = policy_weight(q, row, w_all, w_in, few);
+        const double w = uniform(policy_weight(q, row, w_all, w_in, few));
         T *const d = q.grad ? (T *)q.grad + (int64_t)row * q.grad_ld : nullptr;
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
         const bool same = EXACT && policy_mis(y) == mis, vec = d && policy_mis(d) == mis;
         const bool live = w != 0.0;
         PolicyRow r{};
-        float xa = 0.f;
-        if (live) { r = policy_inputs(q, row, w, tid == 0); xa = ld(x + r.a); }
+        if (live) r = policy_inputs(q, row, w, tid == 0);
         auto piece = [&](const T *v, bool aligned, int j) {
             return aligned && j >= 0 && j + V <= A ? *(const uint4 *)(v + j) : j < A ? policy_edge(v, j, A) : policy_none<T>();
         };
-        float m[2] = {PL_LOWEST, PL_LOWEST}, s[4] = {0.f, 0.f, 0.f, 0.f};
+        PolicyRunning<EXACT, true> u(k);
+        float xa = 0.f;
         if (live)
-            for (int j0 = tid * V - mis; j0 < A; j0 += PL_PIECES * PL_STREAM * V) {
-                uint4 rx[PL_PIECES], ry[PL_PIECES];
+            for (int j0 = tid * V - mis; j0 < A; j0 += CH * BLOCK * V) {
+                uint4 rx[CH], ry[CH];
 #pragma unroll
-                for (int c = 0; c < PL_PIECES; ++c) {
-                    const int j = j0 + c * PL_STREAM * V;
+                for (int c = 0; c < CH; ++c) {
+                    const int j = j0 + c * BLOCK * V;
                     rx[c] = piece(x, true, j);
                     if (EXACT) ry[c] = piece(y, same, j);
                 }
-                float n[2] = {m[0], m[1]};
+                float n[2] = {u.m[0], u.m[1]};
 #pragma unroll
-                for (int c = 0; c < PL_PIECES; ++c) P::max(rx[c], ry[c], n);
-                const float up = (m[0] - n[0]) * k, f = __builtin_amdgcn_exp2f(up);      // (m = n = lowest: 0 and 1)
-                if (EXACT) s[3] = s[0] > 0.f ? s[3] + s[0] * (up - (m[1] - n[1]) * k) : 0.f;
-                s[1] = __builtin_fmaf(s[0], fmaxf(up, PL_ZERO), s[1]);
-                s[0] *= f; s[1] *= f; s[3] *= f;
-                if (EXACT) s[2] *= __builtin_amdgcn_exp2f((m[1] - n[1]) * k);
-                m[0] = n[0]; m[1] = n[1];
+                for (int c = 0; c < CH; ++c) P::max(rx[c], ry[c], r.a - (j0 + c * BLOCK * V), n, xa);
+                u.turn(n);
 #pragma unroll
-                for (int c = 0; c < PL_PIECES; ++c) P::sums(rx[c], ry[c], m[0], m[1], k, s);
+                for (int c = 0; c < CH; ++c) P::sums(rx[c], ry[c], u.z, u.zr, u.s);
             }
-        float top[2] = {m[0], m[1]};
-        row_reduce<PL_STREAM>(top, OpMaxF(), s_max);
-        {
-            const float up = (m[0] - top[0]) * k, upr = (m[1] - top[1]) * k, f = __builtin_amdgcn_exp2f(up);
-            if (EXACT) s[3] = s[0] > 0.f ? s[3] + s[0] * (up - upr) : 0.f;
-            s[1] = __builtin_fmaf(s[0], fmaxf(up, PL_ZERO), s[1]) * f;
-            s[0] *= f; s[3] *= f;
-            if (EXACT) s[2] *= __builtin_amdgcn_exp2f(upr);
-        }
-        row_reduce<PL_STREAM>(s, OpAddF(), s_sum);
-        PolicyCoef c = policy_row(pc, r, PolicySums{s[0], s[2], s[1], s[3]}, xa - top[0], q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
-        const bool dead = !live || s[0] == 0.f;
+        float top[2] = {u.m[0], u.m[1]};
+        reduce_some<BLOCK, EXACT, 2>(top, OpMaxF(), s_max);
+        u.turn(top);
+        u.s[4] = xa;
+        reduce_some<BLOCK, EXACT, 5>(u.s, OpAddF(), s_sum);
+        PolicyCoef c = policy_row(pc, r, PolicySums{u.s[0], u.s[2], u.s[1], u.s[3], u.s[4]}, u.m[0], 0.f, q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
+        if (u.s[0] != u.s[0]) u.z.c = NAN;
+        const bool dead = !live || u.s[0] == 0.f;
         if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
         if (tid == 0) {
             if (q.logp) q.logp[row] = c.logp;
@@ -469,19 +662,19 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
             sum[3] += w * (double)c.clipped;
         }
         if (d)
-            for (int j0 = tid * V - mis; j0 < A; j0 += PL_PIECES * PL_STREAM * V) {
-                uint4 rx[PL_PIECES], ry[PL_PIECES];
+            for (int j0 = tid * V - mis; j0 < A; j0 += CH * BLOCK * V) {
+                uint4 rx[CH], ry[CH];
 #pragma unroll
-                for (int i = 0; i < PL_PIECES; ++i) {
-                    const int j = j0 + i * PL_STREAM * V;
+                for (int i = 0; i < CH; ++i) {
+                    const int j = j0 + i * BLOCK * V;
                     rx[i] = dead ? policy_none<T>() : piece(x, true, j);
                     if (EXACT) ry[i] = dead ? policy_none<T>() : piece(y, same, j);
                 }
 #pragma unroll
-                for (int i = 0; i < PL_PIECES; ++i) {
-                    const int j = j0 + i * PL_STREAM * V;
+                for (int i = 0; i < CH; ++i) {
+                    const int j = j0 + i * BLOCK * V;
                     float o[V];
-                    P::grad(rx[i], ry[i], top[0], top[1], k, c, r.a - j, o);
+                    P::grad(rx[i], ry[i], u.z, u.zr, c, r.a - j, o);
                     if (j < A) policy_put(d, o, j, A, vec);
                 }
             }
@@ -521,11 +714,17 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
 template <class T, bool EXACT>
 static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)
 {
+    constexpr bool HEAVY = EXACT && sizeof(T) == 2;
     const int64_t pieces = q.pieces;
     int grid = 0;
     auto go = [&](auto kern, int block, int per) {
         const int64_t n = ((int64_t)rows + per - 1) / per;
         grid = (int)(n < PL_GRID ? n : PL_GRID);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
+    };
+    auto ring = [&](auto kern, int block) {                         // as many workgroups as fit the chip: 16 waves per CU
+        const int cus = device_cus(), fit = (cus > 0 ? cus : 256) * (1024 / block);
+        grid = rows < fit ? rows : fit;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
     };
 #define HELD(L, C) go(k_policy_held<T, EXACT, L, C>, L > PL_BLOCK ? L : PL_BLOCK, (L > PL_BLOCK ? L : PL_BLOCK) / L)
@@ -535,12 +734,14 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
     else if (pieces <= 64) HELD(16, 4);
     else if (pieces <= 128) HELD(32, 4);
     else if (pieces <= 256) HELD(64, 4);
+    else if (pieces <= 512) HELD(64, 8);
     else if (pieces <= 1024) HELD(256, 4);
     else if (pieces <= 2048) HELD(256, 8);
     else if (pieces <= 4096) HELD(512, 8);
-    else if (pieces <= 8192) HELD(1024, 8);
-    else if (!EXACT && pieces <= 16384) HELD(1024, (EXACT ? 8 : 16));
-    else go(k_policy_stream<T, EXACT>, PL_STREAM, 1);
+    else if (!EXACT && pieces <= 8192) ring(k_policy_ring<T, EXACT, (EXACT ? 1024 : 512), (EXACT ? 8 : 16)>, 512);
+    else if (HEAVY) go(k_policy_stream<T, EXACT, (HEAVY ? 512 : 1024), (HEAVY ? 4 : 2)>, 512, 1);
+    else if (pieces <= (EXACT ? 8192 : 16384)) ring(k_policy_ring<T, EXACT, 1024, (EXACT ? 8 : 16)>, 1024);
+    else go(k_policy_stream<T, EXACT, (HEAVY ? 512 : 1024), (HEAVY ? 4 : 2)>, 1024, 1);
 #undef HELD
     return grid;
 }
@@ -558,8 +759,8 @@ void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStre
     q.by_schedule = g.by_schedule;
     double *partial = (double *)scratch, *w = partial + 4 * PL_GRID;
     int32_t *n = (int32_t *)(w + q.B);
-    const PolicyScalars pc{1.0 / g.temperature, log(1.0 - g.clip_low), log(1.0 + g.clip_high), 1.0 - g.clip_low, 1.0 + g.clip_high,
-                           g.kl_coef, g.entropy_coef, g.scale};
+    const PolicyScalars pc{1.0 / g.temperature, log(1.0 - g.clip_low), log(1.0 + g.clip_high), g.scale / g.temperature, g.kl_coef,
+                           g.entropy_coef, g.scale, (float)(1.0 - g.clip_low), (float)(1.0 + g.clip_high)};
     const double w_all = 1.0 / ((double)q.B * q.G * q.T);           // every step counts: both means are one
     const bool few = (int64_t)q.B * q.T <= PL_FEW && q.B <= PL_INPUTS;
     if (q.eff && !few) {

@@ -4,7 +4,11 @@ Tolerances, derived: with t_j = (x_j - m) log2(e) / temperature, e_j = 2^t_j car
 ln2 * 3 * 2^-24 |t_j| relative, plus one step of 2^x; a sum of A terms at most min(A, 600) additions in one lane (and 16 across lanes)
 plus the errors of its terms; a coefficient at most 16 further roundings. A gradient is a sum of products of these, so its error is at
 most R * 2^-24 times the sum of the magnitudes it is made of (the oracle's `size`), R = 2 * 2.1 * max|t| + min(A, 600) + 48, plus half a
-step of its type. Elements whose |t| is over 60 have p < 2^-60 and are held to that share of their row."""
+step of its type. Elements whose |t| is over 60 have p < 2^-60 and are held to that share of their row.
+The term m log2(e) / temperature in t is itself rounded: every t of a row is off by the same amount, at most 2^-24 |m| log2(e) / temperature =
+2^-24 M. It cancels in p, H and KL, but not in the roundings of the sums and products that hold it: at most 16 of 2^-23 each, so that
+2^-43 M (times weights and coefficients below 1) remains also where all true terms are 0, as for a single action. Rows with M > 2^22 are
+centred before, and have no such term."""
 import numpy as np
 import pytest
 import torch
@@ -81,6 +85,8 @@ def _rel(x, kw):
 def _check(got, ref, x, kw, rel):
     half = HALF[x.dtype]
     tol = rel * ref["size"] + half * np.abs(ref["grad"]) + 2.0 ** -60 * ref["size"].max(-1, keepdims=True) + 1e-37
+    m = np.abs(np.nan_to_num(host(x).astype(np.float64).max(-1, keepdims=True), posinf=0.0, neginf=0.0)) * 1.4427 / kw.get("temperature", 1.0)
+    tol = tol + 2.0 ** -43 * np.where(m > 2.0 ** 22, 0.0, m)
     bad = np.abs(host(got["grad"]).astype(np.float64) - ref["grad"]) > tol
     assert not bad.any(), (bad.sum(), np.argwhere(bad)[:3].tolist())
     np.testing.assert_allclose(host(got["logp"]), ref["logp"], rtol=2.0 ** -23, atol=rel)
@@ -165,6 +171,31 @@ def test_masks(ctx, A, dtype, kl):
     assert np.isfinite(host(got["grad"])).all() and np.isfinite(host(got["stats"])).all()
     kw["adv"][:, :, 1] = 0
     _check(got, ref, x, kw, _rel(x, kw) + 64 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("A", [5, 64, 700, 5000, 40001, 70001, 140001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["none", "logits"])
+def test_rows_far_from_zero(ctx, A, dtype, kl):
+    """Maxima of either sign and any size beside ordinary rows: the softmax does not depend on where its logits lie."""
+    x, ids, kw = _case(1, 2, 6, A, dtype, kl=kl, seed=13)
+    base = x.float()
+    for t, at in enumerate((1e5, -1e5, 2.0 ** 23, -2.0 ** 23, 1e30, -3e38)):
+        moved = (base[:, 0, t] + at).to(dtype)
+        if abs(at) >= 2.0 ** 23:
+            moved = torch.where(torch.arange(A, device="cuda") % 3 == 0, moved, moved - (2 ** 23 if abs(at) < 1e30 else 2.0 ** 90))
+        x[:, 0, t] = moved
+        if kl == "logits":
+            kw["ref_logits"][:, 0, (t + 1) % 6] = x[:, 0, t]
+            kw["ref_logits"][:, 1, t] = x[:, 0, t]
+            x[:, 1, t] = x[:, 0, t]
+    got, ref = _run(ctx, x, ids, {**kw, "old_logp": None}), _oracle(x, ids, {**kw, "old_logp": None})
+    finite = np.isfinite(ref["size"]).all(-1, keepdims=True) & (np.abs(ref["logp"]) < 1e6)[..., None]
+    tol = _rel(x, kw) * ref["size"] + HALF[dtype] * np.abs(ref["grad"]) + 2.0 ** -60 * ref["size"].max(-1, keepdims=True) + 2.0 ** -43 * 2.0 ** 22
+    assert finite.sum() >= 2
+    assert (np.abs(host(got["grad"]) - ref["grad"]) <= tol)[np.broadcast_to(finite, tol.shape)].all()
+    some = np.abs(ref["logp"]) < 1e6
+    np.testing.assert_allclose(host(got["logp"])[some], ref["logp"][some], rtol=2.0 ** -23, atol=_rel(x, kw))
 
 
 @pytest.mark.parametrize("A", [6, 300, 9000, 140001])
