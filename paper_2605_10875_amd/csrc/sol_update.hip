@@ -10,10 +10,10 @@ namespace sol {
 
 constexpr int UP_BLOCK = 256;
 constexpr int UP_GRID = 2048;                                       // workgroups per launch at most
-constexpr int UP_CHUNK = 4096;                                      // elements of one step of a workgroup
+constexpr int UP_STEP = 1024;                                       // elements of one step of a workgroup: four per thread
 constexpr int UP_CLIP = 160, UP_ADAM = 56;                          // tensors per launch (arguments of at most 4 KB)
 
-// first[i]: chunks before tensor i
+// first[i]: steps before tensor i
 struct ClipList { int count; uint32_t first[UP_CLIP + 1]; void *g[UP_CLIP]; int64_t n[UP_CLIP]; };
 struct AdamList {
     int count; uint32_t first[UP_ADAM + 1];
@@ -21,14 +21,47 @@ struct AdamList {
 };
 static_assert(sizeof(ClipList) <= 3600 && sizeof(AdamList) <= 3600, "kernel arguments");
 
-template <class L> __device__ __forceinline__ int tensor_of(const L &l, uint32_t chunk)
+// f(tensor, first element, elements) for the steps blockIdx.x, blockIdx.x + gridDim.x, .. of a list, from its end to its beginning
+// where BACK: what the pass before read last is then still in the caches.
+template <bool BACK, class L, class F> __device__ __forceinline__ void each_step(const L &l, F f)
 {
-    int lo = 0, hi = l.count;                                       // first[lo] <= chunk < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (l.first[mid] <= chunk) lo = mid; else hi = mid;
+    const uint32_t steps = l.first[l.count];
+    int lo = 0, hi = l.count;                                       // first[lo] <= step < first[hi]
+    for (uint32_t k = blockIdx.x; k < steps; k += gridDim.x) {
+        const uint32_t c = BACK ? steps - 1 - k : k;
+        if (BACK) lo = 0; else hi = l.count;                        // steps come in order: one end of the bracket stays
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (l.first[mid] <= c) lo = mid; else hi = mid;
+        }
+        const int64_t at = (int64_t)(c - l.first[lo]) * UP_STEP, left = l.n[lo] - at;
+        f(lo, at, (int)(left < UP_STEP ? left : UP_STEP));
     }
-    return lo;
+}
+
+// Four consecutive elements of a thread. A pointer's phase is its distance from a boundary of four elements: where all streams of a tensor
+// have one, its elements are taken from the boundaries on in single accesses of 8 or 16 bytes, else one by one.
+template <class T> struct Four;
+template <> struct Four<float> {
+    static __device__ __forceinline__ void load(const float *p, float (&f)[4]) { const float4 v = *(const float4 *)p; f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+    static __device__ __forceinline__ void store(float *p, const float (&f)[4]) { *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Four<bf16_t> {
+    static __device__ __forceinline__ void load(const bf16_t *p, float (&f)[4])
+    {
+        const uint2 v = *(const uint2 *)p;
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void store(bf16_t *p, const float (&f)[4]) { *(uint2 *)p = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])); }
+};
+template <class T> __device__ __forceinline__ int phase(const T *p) { return (int)((uintptr_t)p / sizeof(T) & 3); }
+
+// A step's last `ph` elements lie behind its last thread's four: the one that this thread takes, -1 if none
+__device__ __forceinline__ int last_ones(int ph, int n)
+{
+    const int e = UP_STEP - ph + (int)threadIdx.x;
+    return (int)threadIdx.x < ph && e < n ? e : -1;
 }
 
 __device__ __forceinline__ double up_block_sum(double v, double *red)
@@ -43,18 +76,26 @@ __device__ __forceinline__ double up_block_sum(double v, double *red)
     return t;
 }
 
-// Squares are summed in 64 bits: neither do they overflow, nor does the number of elements show.
+// Squares are summed in 64 bits: neither do they overflow, nor does the number of elements show. Bound by reading the gradients once.
 template <class T>
 __global__ void __launch_bounds__(UP_BLOCK) k_grad_squares(ClipList l, double *__restrict__ partial)
 {
     __shared__ double red[UP_BLOCK / 64];
     double s = 0.0;
-    for (uint32_t c = blockIdx.x; c < l.first[l.count]; c += gridDim.x) {
-        const int i = tensor_of(l, c);
-        const T *const g = (const T *)l.g[i];
-        const int64_t at = (int64_t)(c - l.first[i]) * UP_CHUNK, end = at + UP_CHUNK < l.n[i] ? at + UP_CHUNK : l.n[i];
-        for (int64_t j = at + threadIdx.x; j < end; j += UP_BLOCK) { const double x = (double)ld(g + j); s += x * x; }
-    }
+    each_step<false>(l, [&](int i, int64_t at, int n) {
+        const T *const g = (const T *)l.g[i] + at;
+        const int j = (int)threadIdx.x * 4 - phase(g);              // its four elements; those before the step belong to the one before
+        if (j >= 0 && j + 4 <= n) {
+            float f[4];
+            Four<T>::load(g + j, f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_fma((double)f[e], (double)f[e], s);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) { const double x = (double)ld(g + j + e); s += x * x; }
+        }
+        if (const int e = last_ones(phase(g), n); e >= 0) { const double x = (double)ld(g + e); s += x * x; }
+    });
     s = up_block_sum(s, red);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -79,12 +120,21 @@ __global__ void __launch_bounds__(UP_BLOCK) k_grad_scale(ClipList l, const float
 {
     const float f = *coef;
     if (!(f < 1.f)) return;
-    for (uint32_t c = blockIdx.x; c < l.first[l.count]; c += gridDim.x) {
-        const int i = tensor_of(l, c);
-        T *const g = (T *)l.g[i];
-        const int64_t at = (int64_t)(c - l.first[i]) * UP_CHUNK, end = at + UP_CHUNK < l.n[i] ? at + UP_CHUNK : l.n[i];
-        for (int64_t j = at + threadIdx.x; j < end; j += UP_BLOCK) st(g + j, ld(g + j) * f);
-    }
+    each_step<true>(l, [&](int i, int64_t at, int n) {
+        T *const g = (T *)l.g[i] + at;
+        const int ph = phase(g), j = (int)threadIdx.x * 4 - ph;
+        if (j >= 0 && j + 4 <= n) {
+            float x[4];
+            Four<T>::load(g + j, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] *= f;
+            Four<T>::store(g + j, x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) st(g + j + e, ld(g + j + e) * f);
+        }
+        if (const int e = last_ones(ph, n); e >= 0) st(g + e, ld(g + e) * f);
+    });
 }
 
 // b^t by squaring
@@ -107,20 +157,42 @@ k_adamw(AdamList l, AdamCfg a, const int32_t *__restrict__ step, const float *__
     const float b1 = (float)a.beta1, c1 = (float)(1.0 - a.beta1), b2 = (float)a.beta2, c2 = (float)(1.0 - a.beta2);
     const float keep = (float)(1.0 - lr * a.weight_decay), rate = (float)(lr / (1.0 - pow_int(a.beta1, t)));
     const float corr = (float)(1.0 / (1.0 - pow_int(a.beta2, t))), eps = (float)a.eps;
-    for (uint32_t c = blockIdx.x; c < l.first[l.count]; c += gridDim.x) {
-        const int i = tensor_of(l, c);
-        float *const p = l.p[i], *const m = l.m[i], *const v = l.v[i];
-        const T *const g = (const T *)l.g[i];
-        bf16_t *const copy = l.copy[i];
-        const int64_t at = (int64_t)(c - l.first[i]) * UP_CHUNK, end = at + UP_CHUNK < l.n[i] ? at + UP_CHUNK : l.n[i];
-        for (int64_t j = at + threadIdx.x; j < end; j += UP_BLOCK) {
-            const float x = ld(g + j) * scale;
-            const float mn = b1 * m[j] + c1 * x, vn = b2 * v[j] + c2 * x * x;
-            const float pn = p[j] * keep - rate * mn / (sqrtf(vn * corr) + eps);
-            m[j] = mn; v[j] = vn; p[j] = pn;
-            if (copy) copy[j] = f32_to_bf16(pn);
+    auto one = [&](float x, float &p, float &m, float &v) {
+        x *= scale;
+        m = b1 * m + c1 * x;
+        v = b2 * v + c2 * x * x;
+        p = p * keep - rate * m / (sqrtf(v * corr) + eps);
+    };
+    each_step<true>(l, [&](int i, int64_t at, int n) {
+        float *const p = l.p[i] + at, *const m = l.m[i] + at, *const v = l.v[i] + at;
+        const T *const g = (const T *)l.g[i] + at;
+        bf16_t *const copy = l.copy[i] ? l.copy[i] + at : nullptr;
+        const int ph = phase(p);
+        auto single = [&](int j) {
+            float pj = p[j], mj = m[j], vj = v[j];
+            one(ld(g + j), pj, mj, vj);
+            p[j] = pj; m[j] = mj; v[j] = vj;
+            if (copy) copy[j] = f32_to_bf16(pj);
+        };
+        if (phase(m) == ph && phase(v) == ph && phase(g) == ph && (!copy || phase(copy) == ph)) {
+            const int j = (int)threadIdx.x * 4 - ph;
+            if (j >= 0 && j + 4 <= n) {
+                float pf[4], mf[4], vf[4], gf[4];
+                Four<float>::load(p + j, pf); Four<float>::load(m + j, mf); Four<float>::load(v + j, vf); Four<T>::load(g + j, gf);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) one(gf[e], pf[e], mf[e], vf[e]);
+                Four<float>::store(m + j, mf); Four<float>::store(v + j, vf); Four<float>::store(p + j, pf);
+                if (copy) Four<bf16_t>::store(copy + j, pf);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) single(j + e);
+            }
+            if (const int e = last_ones(ph, n); e >= 0) single(e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (const int j = (int)threadIdx.x + e * UP_BLOCK; j < n) single(j);
         }
-    }
+    });
 }
 
 // The list in parts of at most CAP tensors of one type: f(type, part, workgroups).
@@ -130,18 +202,18 @@ static void in_parts(const Item *items, int count, Put put, F f)
     for (int dtype = 0; dtype < 2; ++dtype) {
         List l;
         l.count = 0;
-        uint64_t chunks = 0;
+        uint64_t steps = 0;
         auto flush = [&] {
-            if (l.count) { l.first[l.count] = (uint32_t)chunks; f(dtype, l, (int)(chunks < UP_GRID ? chunks : UP_GRID)); }
-            l.count = 0; chunks = 0;
+            if (l.count) { l.first[l.count] = (uint32_t)steps; f(dtype, l, (int)(steps < UP_GRID ? steps : UP_GRID)); }
+            l.count = 0; steps = 0;
         };
         for (int i = 0; i < count; ++i) {
             if (items[i].dtype != dtype || items[i].n == 0) continue;
-            const uint64_t c = (uint64_t)((items[i].n + UP_CHUNK - 1) / UP_CHUNK);
-            if (l.count == CAP || chunks + c > 0x7fffffffu) flush();
-            l.first[l.count] = (uint32_t)chunks;
+            const uint64_t c = (uint64_t)((items[i].n + UP_STEP - 1) / UP_STEP);
+            if (l.count == CAP || steps + c > 0x7fffffffu) flush();
+            l.first[l.count] = (uint32_t)steps;
             put(l, l.count, items[i]);
-            chunks += c; ++l.count;
+            steps += c; ++l.count;
         }
         flush();
     }
