@@ -952,10 +952,15 @@ static int launched(sol_ctx *ctx)
 struct Range { uintptr_t from, to; };                          // bytes [from, to)
 static Range range_of(const void *p, uint64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + bytes}; }
 static bool meet(const Range &a, const Range &b) { return a.from < b.to && b.from < a.to; }
-// whether any two of them meet (sorts them)
-static bool any_meet(std::vector<Range> &r)
+// Sorts ranges that come in runs of `run` entries, most often each in order already (views into one buffer), and says whether any two meet.
+static bool any_meet(std::vector<Range> &r, size_t run)
 {
-    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
+    auto before = [](const Range &a, const Range &b) { return a.from < b.from; };
+    for (size_t i = 0; i < r.size(); i += run) {
+        const auto from = r.begin() + (ptrdiff_t)i, to = r.begin() + (ptrdiff_t)std::min(i + run, r.size());
+        if (!std::is_sorted(from, to, before)) std::sort(from, to, before);
+        if (i) std::inplace_merge(r.begin(), from, to, before);
+    }
     for (size_t i = 1; i < r.size(); ++i) if (r[i].from < r[i - 1].to) return true;
     return false;
 }
@@ -1037,14 +1042,14 @@ static int grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double 
     at.reserve((size_t)n_tensors);
     for (int i = 0; i < n_tensors; ++i) {
         const sol_grad &g = grads[i];
-        const std::string which = "gradient " + std::to_string(i);
-        if (g.n < 0 || (g.n > 0 && !g.data)) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": no data");
-        if (g.dtype != SOL_F32 && g.dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": dtype must be SOL_F32 or SOL_BF16");
-        if ((uintptr_t)g.data % esize(g.dtype)) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": not aligned to its elements");
+        auto which = [i] { return "gradient " + std::to_string(i); };
+        if (g.n < 0 || (g.n > 0 && !g.data)) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": no data");
+        if (g.dtype != SOL_F32 && g.dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": dtype must be SOL_F32 or SOL_BF16");
+        if ((uintptr_t)g.data % esize(g.dtype)) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": not aligned to its elements");
         items[i] = GradItem{g.data, g.n, g.dtype};
         if (g.n) at.push_back(range_of(g.data, (uint64_t)g.n * esize(g.dtype)));
     }
-    if (scale_grads && any_meet(at)) return fail(ctx, SOL_ERR_INVALID_ARG, "two gradients overlap");
+    if (scale_grads && any_meet(at, at.size())) return fail(ctx, SOL_ERR_INVALID_ARG, "two gradients overlap");
     const size_t need = sol_grad_clip_workspace_bytes(n_tensors);
     if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
     if (const int rc = on_device(ctx)) return rc;
@@ -1078,18 +1083,22 @@ static int adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tenso
     read.reserve((size_t)n_tensors);
     for (int i = 0; i < n_tensors; ++i) {
         const sol_adamw_tensor &t = tensors[i];
-        const std::string which = "tensor " + std::to_string(i);
-        if (t.n < 0 || (t.n > 0 && (!t.param || !t.m || !t.v || !t.grad))) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": no data");
-        if (t.grad_dtype != SOL_F32 && t.grad_dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which + ": grad_dtype must be SOL_F32 or SOL_BF16");
+        auto which = [i] { return "tensor " + std::to_string(i); };
+        if (t.n < 0 || (t.n > 0 && (!t.param || !t.m || !t.v || !t.grad))) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": no data");
+        if (t.grad_dtype != SOL_F32 && t.grad_dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": grad_dtype must be SOL_F32 or SOL_BF16");
         if (((uintptr_t)t.param | (uintptr_t)t.m | (uintptr_t)t.v) % 4 || (uintptr_t)t.grad % esize(t.grad_dtype) || (uintptr_t)t.copy % 2)
-            return fail(ctx, SOL_ERR_INVALID_ARG, which + ": not aligned to its elements");
+            return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": not aligned to its elements");
         items[i] = AdamItem{t.param, t.m, t.v, t.grad, t.copy, t.n, t.grad_dtype};
         if (!t.n) continue;
-        for (const float *p : {t.param, t.m, t.v}) at.push_back(range_of(p, 4 * (uint64_t)t.n));
-        if (t.copy) at.push_back(range_of(t.copy, 2 * (uint64_t)t.n));
         read.push_back(range_of(t.grad, (uint64_t)t.n * esize(t.grad_dtype)));
     }
-    if (any_meet(at)) return fail(ctx, SOL_ERR_INVALID_ARG, "two of the tensors to be written overlap");
+    for (int k = 0; k < 4; ++k)
+        for (int i = 0; i < n_tensors; ++i) {
+            const sol_adamw_tensor &t = tensors[i];
+            const void *const p = k == 0 ? t.param : k == 1 ? t.m : k == 2 ? (const void *)t.v : t.copy;
+            if (t.n && p) at.push_back(range_of(p, (k == 3 ? 2 : 4) * (uint64_t)t.n));
+        }
+    if (any_meet(at, (size_t)n_tensors)) return fail(ctx, SOL_ERR_INVALID_ARG, "two of the tensors to be written overlap");
     for (const Range &g : read) {                               // a gradient may serve two tensors, but nothing is written into it
         const auto after = std::lower_bound(at.begin(), at.end(), g.to, [](const Range &r, uintptr_t v) { return r.from < v; });
         if (after != at.begin() && meet(*(after - 1), g)) return fail(ctx, SOL_ERR_INVALID_ARG, "a gradient overlaps a tensor to be written");

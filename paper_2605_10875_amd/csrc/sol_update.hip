@@ -9,21 +9,26 @@
 namespace sol {
 
 constexpr int UP_BLOCK = 256;
-constexpr int UP_GRID = 2048;                                       // workgroups per launch at most
-constexpr int UP_STEP = 1024;                                       // elements of one step of a workgroup: four per thread
-constexpr int UP_CLIP = 160, UP_ADAM = 56;                          // tensors per launch (arguments of at most 4 KB)
+constexpr int UP_PARTS = 2048;                                      // workgroups of the norm per launch at most, each with a partial sum
+constexpr uint64_t UP_STEPS = 0xffffff;                             // steps of a launch at most: 2^32 threads
+constexpr int UP_VECS = 4;                                          // accesses of 16 bytes in flight per thread, for norm and scaling
+constexpr int UP_STEP = 1024;                                       // elements of one step of an update's workgroup: four per thread
+// elements of one step of a norm's or scaling's workgroup
+template <class T> constexpr int clip_step() { return UP_BLOCK * UP_VECS * Vec16<T>::N; }
+constexpr int UP_CLIP = 240, UP_ADAM = 80;                          // tensors per launch (arguments of at most 4 KB)
+constexpr int64_t UP_LONGEST = (int64_t)1 << 31;                    // a longer tensor takes several places of a list
 
 // first[i]: steps before tensor i
-struct ClipList { int count; uint32_t first[UP_CLIP + 1]; void *g[UP_CLIP]; int64_t n[UP_CLIP]; };
+struct ClipList { int count; uint32_t first[UP_CLIP + 1]; void *g[UP_CLIP]; uint32_t n[UP_CLIP]; };
 struct AdamList {
     int count; uint32_t first[UP_ADAM + 1];
-    float *p[UP_ADAM], *m[UP_ADAM], *v[UP_ADAM]; const void *g[UP_ADAM]; bf16_t *copy[UP_ADAM]; int64_t n[UP_ADAM];
+    float *p[UP_ADAM], *m[UP_ADAM], *v[UP_ADAM]; const void *g[UP_ADAM]; bf16_t *copy[UP_ADAM]; uint32_t n[UP_ADAM];
 };
-static_assert(sizeof(ClipList) <= 3600 && sizeof(AdamList) <= 3600, "kernel arguments");
+static_assert(sizeof(ClipList) + 64 <= 4096 && sizeof(AdamList) + 128 <= 4096, "kernel arguments");
 
 // f(tensor, first element, elements) for the steps blockIdx.x, blockIdx.x + gridDim.x, .. of a list, from its end to its beginning
 // where BACK: what the pass before read last is then still in the caches.
-template <bool BACK, class L, class F> __device__ __forceinline__ void each_step(const L &l, F f)
+template <bool BACK, int STEP, class L, class F> __device__ __forceinline__ void each_step(const L &l, F f)
 {
     const uint32_t steps = l.first[l.count];
     int lo = 0, hi = l.count;                                       // first[lo] <= step < first[hi]
@@ -34,12 +39,12 @@ template <bool BACK, class L, class F> __device__ __forceinline__ void each_step
             const int mid = (lo + hi) >> 1;
             if (l.first[mid] <= c) lo = mid; else hi = mid;
         }
-        const int64_t at = (int64_t)(c - l.first[lo]) * UP_STEP, left = l.n[lo] - at;
-        f(lo, at, (int)(left < UP_STEP ? left : UP_STEP));
+        const int64_t at = (int64_t)(c - l.first[lo]) * STEP, left = (int64_t)l.n[lo] - at;
+        f(lo, at, (int)(left < STEP ? left : STEP));
     }
 }
 
-// Four consecutive elements of a thread. A pointer's phase is its distance from a boundary of four elements: where all streams of a tensor
+// Four consecutive elements of a thread. A pointer's phase is its distance from a boundary of N elements: where all streams of a tensor
 // have one, its elements are taken from the boundaries on in single accesses of 8 or 16 bytes, else one by one.
 template <class T> struct Four;
 template <> struct Four<float> {
@@ -55,23 +60,42 @@ template <> struct Four<bf16_t> {
     }
     static __device__ __forceinline__ void store(bf16_t *p, const float (&f)[4]) { *(uint2 *)p = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])); }
 };
-template <class T> __device__ __forceinline__ int phase(const T *p) { return (int)((uintptr_t)p / sizeof(T) & 3); }
+template <int N, class T> __device__ __forceinline__ int phase(const T *p) { return (int)((uintptr_t)p / sizeof(T) & (N - 1)); }
 
-// A step's last `ph` elements lie behind its last thread's four: the one that this thread takes, -1 if none
-__device__ __forceinline__ int last_ones(int ph, int n)
+// A step's last `ph` elements lie behind its last thread's: the one that this thread takes, -1 if none
+template <int STEP> __device__ __forceinline__ int last_ones(int ph, int n)
 {
-    const int e = UP_STEP - ph + (int)threadIdx.x;
+    const int e = STEP - ph + (int)threadIdx.x;
     return (int)threadIdx.x < ph && e < n ? e : -1;
 }
 
-__device__ __forceinline__ double up_block_sum(double v, double *red)
+// One step of one stream, UP_VECS accesses of 16 bytes per thread: whole(vector index, element) for those that lie inside, single(element)
+// for the elements of the others
+template <class T, class W, class S> __device__ __forceinline__ void stream_step(int ph, int n, W whole, S single)
+{
+    constexpr int V = Vec16<T>::N;
+    const int j0 = (int)threadIdx.x * V - ph;
+    static_for<UP_VECS>([&](auto v) {
+        const int j = j0 + (int)v * UP_BLOCK * V;
+        if (j >= 0 && j + V <= n) whole(v, j);
+    });
+#pragma unroll 1
+    for (int v = 0; v < UP_VECS; ++v) {
+        const int j = j0 + v * UP_BLOCK * V;
+        if (j < n && (j < 0 || j + V > n))
+            for (int e = 0; e < V; ++e) if (j + e >= 0 && j + e < n) single(j + e);
+    }
+    if (const int e = last_ones<clip_step<T>()>(ph, n); e >= 0) single(e);
+}
+
+template <int BLOCK> __device__ __forceinline__ double up_block_sum(double v, double *red)
 {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     double t = 0.0;
 #pragma unroll
-    for (int i = 0; i < UP_BLOCK / 64; ++i) t += red[i];
+    for (int i = 0; i < BLOCK / 64; ++i) t += red[i];
     __syncthreads();
     return t;
 }
@@ -82,32 +106,34 @@ __global__ void __launch_bounds__(UP_BLOCK) k_grad_squares(ClipList l, double *_
 {
     __shared__ double red[UP_BLOCK / 64];
     double s = 0.0;
-    each_step<false>(l, [&](int i, int64_t at, int n) {
+    each_step<false, clip_step<T>()>(l, [&](int i, int64_t at, int n) {
         const T *const g = (const T *)l.g[i] + at;
-        const int j = (int)threadIdx.x * 4 - phase(g);              // its four elements; those before the step belong to the one before
-        if (j >= 0 && j + 4 <= n) {
-            float f[4];
-            Four<T>::load(g + j, f);
+        Vec16<T> x[UP_VECS];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_fma((double)f[e], (double)f[e], s);
-        } else {
+        for (int v = 0; v < UP_VECS; ++v) x[v].raw = {};
+        stream_step<T>(phase<Vec16<T>::N>(g), n, [&](auto v, int j) { x[v].load(g + j); },
+                       [&](int j) { const double f = (double)ld(g + j); s = __builtin_fma(f, f, s); });
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) { const double x = (double)ld(g + j + e); s += x * x; }
+        for (int v = 0; v < UP_VECS; ++v) {
+            float f[Vec16<T>::N];
+            x[v].unpack(f);
+#pragma unroll
+            for (int e = 0; e < Vec16<T>::N; ++e) s = __builtin_fma((double)f[e], (double)f[e], s);
         }
-        if (const int e = last_ones(phase(g), n); e >= 0) { const double x = (double)ld(g + e); s += x * x; }
     });
-    s = up_block_sum(s, red);
+    s = up_block_sum<UP_BLOCK>(s, red);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
 // coef is NaN where the norm is not finite: scaling and update then leave everything as it is
-__global__ void __launch_bounds__(UP_BLOCK)
+__global__ void __launch_bounds__(1024)
 k_grad_norm(const double *__restrict__ partial, int64_t n, double max_norm, double eps, float *__restrict__ norm, float *__restrict__ coef)
 {
-    __shared__ double red[UP_BLOCK / 64];
+    __shared__ double red[1024 / 64];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += UP_BLOCK) s += partial[i];
-    s = sqrt(up_block_sum(s, red));
+#pragma unroll 2
+    for (int64_t i = threadIdx.x; i < n; i += 1024) s += partial[i];
+    s = sqrt(up_block_sum<1024>(s, red));
     if (threadIdx.x == 0) {
         *norm = (float)s;
         const double c = max_norm / (s + eps);
@@ -120,20 +146,24 @@ __global__ void __launch_bounds__(UP_BLOCK) k_grad_scale(ClipList l, const float
 {
     const float f = *coef;
     if (!(f < 1.f)) return;
-    each_step<true>(l, [&](int i, int64_t at, int n) {
+    each_step<true, clip_step<T>()>(l, [&](int i, int64_t at, int n) {
         T *const g = (T *)l.g[i] + at;
-        const int ph = phase(g), j = (int)threadIdx.x * 4 - ph;
-        if (j >= 0 && j + 4 <= n) {
-            float x[4];
-            Four<T>::load(g + j, x);
+        Vec16<T> x[UP_VECS];
+        const int ph = phase<Vec16<T>::N>(g);
+        stream_step<T>(ph, n, [&](auto v, int j) { x[v].load(g + j); }, [&](int j) { st(g + j, ld(g + j) * f); });
+        const int j0 = (int)threadIdx.x * Vec16<T>::N - ph;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] *= f;
-            Four<T>::store(g + j, x);
-        } else {
+        for (int v = 0; v < UP_VECS; ++v) {
+            const int j = j0 + v * UP_BLOCK * Vec16<T>::N;
+            if (j >= 0 && j + Vec16<T>::N <= n) {
+                float y[Vec16<T>::N];
+                x[v].unpack(y);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) st(g + j + e, ld(g + j + e) * f);
+                for (int e = 0; e < Vec16<T>::N; ++e) y[e] *= f;
+                x[v].pack(y);
+                x[v].store(g + j);
+            }
         }
-        if (const int e = last_ones(ph, n); e >= 0) st(g + e, ld(g + e) * f);
     });
 }
 
@@ -163,18 +193,18 @@ k_adamw(AdamList l, AdamCfg a, const int32_t *__restrict__ step, const float *__
         v = b2 * v + c2 * x * x;
         p = p * keep - rate * m / (sqrtf(v * corr) + eps);
     };
-    each_step<true>(l, [&](int i, int64_t at, int n) {
+    each_step<true, UP_STEP>(l, [&](int i, int64_t at, int n) {
         float *const p = l.p[i] + at, *const m = l.m[i] + at, *const v = l.v[i] + at;
         const T *const g = (const T *)l.g[i] + at;
         bf16_t *const copy = l.copy[i] ? l.copy[i] + at : nullptr;
-        const int ph = phase(p);
+        const int ph = phase<4>(p);
         auto single = [&](int j) {
             float pj = p[j], mj = m[j], vj = v[j];
             one(ld(g + j), pj, mj, vj);
             p[j] = pj; m[j] = mj; v[j] = vj;
             if (copy) copy[j] = f32_to_bf16(pj);
         };
-        if (phase(m) == ph && phase(v) == ph && phase(g) == ph && (!copy || phase(copy) == ph)) {
+        if (phase<4>(m) == ph && phase<4>(v) == ph && phase<4>(g) == ph && (!copy || phase<4>(copy) == ph)) {
             const int j = (int)threadIdx.x * 4 - ph;
             if (j >= 0 && j + 4 <= n) {
                 float pf[4], mf[4], vf[4], gf[4];
@@ -187,7 +217,7 @@ k_adamw(AdamList l, AdamCfg a, const int32_t *__restrict__ step, const float *__
 #pragma unroll
                 for (int e = 0; e < 4; ++e) if (j + e >= 0 && j + e < n) single(j + e);
             }
-            if (const int e = last_ones(ph, n); e >= 0) single(e);
+            if (const int e = last_ones<UP_STEP>(ph, n); e >= 0) single(e);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) if (const int j = (int)threadIdx.x + e * UP_BLOCK; j < n) single(j);
@@ -195,60 +225,68 @@ k_adamw(AdamList l, AdamCfg a, const int32_t *__restrict__ step, const float *__
     });
 }
 
-// The list in parts of at most CAP tensors of one type: f(type, part, workgroups).
-template <class List, int CAP, class Item, class Put, class F>
-static void in_parts(const Item *items, int count, Put put, F f)
+// The list in parts of at most CAP places of one type: put(part, place, tensor, first element, elements), then f(type, part, its steps).
+template <class List, int CAP, class Item, class Step, class Put, class F>
+static void in_parts(const Item *items, int count, Step step, Put put, F f)
 {
     for (int dtype = 0; dtype < 2; ++dtype) {
         List l;
         l.count = 0;
         uint64_t steps = 0;
         auto flush = [&] {
-            if (l.count) { l.first[l.count] = (uint32_t)steps; f(dtype, l, (int)(steps < UP_GRID ? steps : UP_GRID)); }
+            if (l.count) { l.first[l.count] = (uint32_t)steps; f(dtype, l, (int)steps); }
             l.count = 0; steps = 0;
         };
         for (int i = 0; i < count; ++i) {
-            if (items[i].dtype != dtype || items[i].n == 0) continue;
-            const uint64_t c = (uint64_t)((items[i].n + UP_STEP - 1) / UP_STEP);
-            if (l.count == CAP || steps + c > 0x7fffffffu) flush();
-            l.first[l.count] = (uint32_t)steps;
-            put(l, l.count, items[i]);
-            steps += c; ++l.count;
+            if (items[i].dtype != dtype) continue;
+            for (int64_t at = 0; at < items[i].n; at += UP_LONGEST) {
+                const int64_t n = items[i].n - at < UP_LONGEST ? items[i].n - at : UP_LONGEST, c = (n + step(dtype) - 1) / step(dtype);
+                if (l.count == CAP || steps + (uint64_t)c > UP_STEPS) flush();
+                l.first[l.count] = (uint32_t)steps;
+                put(l, l.count, items[i], at, (uint32_t)n);
+                steps += (uint64_t)c; ++l.count;
+            }
         }
         flush();
     }
 }
 
-size_t clip_scratch_bytes(int count) { return ((size_t)count / UP_CLIP + 3) * UP_GRID * sizeof(double); }
+// partial sums of as many launches as `count` tensors can take: 240 places each, one launch more per type, and what tensors of over 2^31
+// elements take besides (fewer than 240 in any memory)
+size_t clip_scratch_bytes(int count) { return ((size_t)count / UP_CLIP + 4) * UP_PARTS * sizeof(double); }
 
 void launch_grad_clip(const GradItem *items, int count, double max_norm, double eps, bool scale, float *norm, float *coef, void *scratch,
                       hipStream_t st)
 {
     double *const partial = (double *)scratch;
     int64_t used = 0;
-    auto put = [](ClipList &l, int i, const GradItem &t) { l.g[i] = t.g; l.n[i] = t.n; };
-    in_parts<ClipList, UP_CLIP>(items, count, put, [&](int dtype, const ClipList &l, int grid) {
+    auto step = [](int dtype) { return dtype == 1 ? clip_step<bf16_t>() : clip_step<float>(); };
+    auto put = [](ClipList &l, int i, const GradItem &t, int64_t at, uint32_t n) { l.g[i] = (char *)t.g + at * (t.dtype == 1 ? 2 : 4); l.n[i] = n; };
+    in_parts<ClipList, UP_CLIP>(items, count, step, put, [&](int dtype, const ClipList &l, int steps) {
+        const int grid = steps < UP_PARTS ? steps : UP_PARTS;
         if (dtype == 1) hipLaunchKernelGGL(k_grad_squares<bf16_t>, dim3(grid), dim3(UP_BLOCK), 0, st, l, partial + used);
         else hipLaunchKernelGGL(k_grad_squares<float>, dim3(grid), dim3(UP_BLOCK), 0, st, l, partial + used);
         used += grid;
     });
-    hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(UP_BLOCK), 0, st, partial, used, max_norm, eps, norm, coef);
+    hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(1024), 0, st, partial, used, max_norm, eps, norm, coef);
     if (scale)
-        in_parts<ClipList, UP_CLIP>(items, count, put, [&](int dtype, const ClipList &l, int grid) {
-            if (dtype == 1) hipLaunchKernelGGL(k_grad_scale<bf16_t>, dim3(grid), dim3(UP_BLOCK), 0, st, l, coef);
-            else hipLaunchKernelGGL(k_grad_scale<float>, dim3(grid), dim3(UP_BLOCK), 0, st, l, coef);
+        in_parts<ClipList, UP_CLIP>(items, count, step, put, [&](int dtype, const ClipList &l, int steps) {
+            if (dtype == 1) hipLaunchKernelGGL(k_grad_scale<bf16_t>, dim3(steps), dim3(UP_BLOCK), 0, st, l, coef);
+            else hipLaunchKernelGGL(k_grad_scale<float>, dim3(steps), dim3(UP_BLOCK), 0, st, l, coef);
         });
 }
 
 void launch_adamw(const AdamItem *items, int count, const AdamCfg &a, const int32_t *step, const float *lr_dev, const float *coef,
                   int *flags, hipStream_t st)
 {
-    auto put = [](AdamList &l, int i, const AdamItem &t) {
-        l.p[i] = t.p; l.m[i] = t.m; l.v[i] = t.v; l.g[i] = t.g; l.copy[i] = (bf16_t *)t.copy; l.n[i] = t.n;
+    auto put = [](AdamList &l, int i, const AdamItem &t, int64_t at, uint32_t n) {
+        l.p[i] = t.p + at; l.m[i] = t.m + at; l.v[i] = t.v + at; l.n[i] = n;
+        l.g[i] = (const char *)t.g + at * (t.dtype == 1 ? 2 : 4);
+        l.copy[i] = t.copy ? (bf16_t *)t.copy + at : nullptr;
     };
-    in_parts<AdamList, UP_ADAM>(items, count, put, [&](int dtype, const AdamList &l, int grid) {
-        if (dtype == 1) hipLaunchKernelGGL(k_adamw<bf16_t>, dim3(grid), dim3(UP_BLOCK), 0, st, l, a, step, lr_dev, coef, flags);
-        else hipLaunchKernelGGL(k_adamw<float>, dim3(grid), dim3(UP_BLOCK), 0, st, l, a, step, lr_dev, coef, flags);
+    in_parts<AdamList, UP_ADAM>(items, count, [](int) { return UP_STEP; }, put, [&](int dtype, const AdamList &l, int steps) {
+        if (dtype == 1) hipLaunchKernelGGL(k_adamw<bf16_t>, dim3(steps), dim3(UP_BLOCK), 0, st, l, a, step, lr_dev, coef, flags);
+        else hipLaunchKernelGGL(k_adamw<float>, dim3(steps), dim3(UP_BLOCK), 0, st, l, a, step, lr_dev, coef, flags);
     });
 }
 

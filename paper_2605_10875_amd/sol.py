@@ -255,13 +255,30 @@ def _row_step(t, what):
     return step
 
 
-def _flat(ts, dtypes, what):
-    """The tensors of a list: contiguous, of one of these types, on the current device."""
-    here = torch.cuda.current_device()
-    for i, t in enumerate(ts):
-        if t.dtype not in dtypes or t.get_device() != here or not t.is_contiguous():
-            raise ValueError(f"{what}[{i}]: a contiguous tensor of {' or '.join(map(str, dtypes))} on the current device is needed")
-    return ts
+_lists = None
+
+
+def _tensor_lists(lists, names, types, typed):
+    """Host array of records for lists of as many tensors each (None: a list that is not there): addresses, elements, type of the
+    list `typed`. types: 1 float32, 2 bfloat16, 3 either."""
+    global _lists
+    if _lists is None:
+        if not os.path.exists(_build.LISTS_LIB):
+            _build.build_lists()
+        L = C.PyDLL(_build.LISTS_LIB)
+        L.sol_tensor_lists.restype = C.c_int64
+        L.sol_tensor_lists.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
+        _lists = L.sol_tensor_lists
+    n, k = len(lists[0]), len(lists)
+    words = (C.c_int64 * (n * (k + 2)))()
+    rc = _lists(lists, n, (C.c_int32 * k)(*types), typed, torch.cuda.current_device(), words)
+    if rc:
+        _need(rc > 0, "the lists have to be sequences of the same length")
+        rc -= 1
+        which, at, kind = rc // 8 % 16, rc // 128, {1: "float32", 2: "bfloat16", 3: "float32 or bfloat16"}
+        raise ValueError(f"{names[which]}[{at}]: " + ("a tensor is needed", f"{kind[types[which]]} is needed", "not on the current device",
+                                                      "a contiguous tensor is needed", f"not as many elements as {names[0]}[{at}]")[rc % 8])
+    return words, n
 
 
 def _used_on(stream, *ts):
@@ -543,42 +560,28 @@ class Sol:
     def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
         """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
         [1] on the device; scale: the gradients are multiplied by coef in place. Nothing is synchronised."""
-        _flat(grads, _CODE, "grads")
-        arr = (C.c_int64 * (3 * len(grads)))(*[v for g in grads for v in (g.data_ptr(), g.numel(), _CODE[g.dtype])])
+        words, n = _tensor_lists((grads,), ("grads",), (3,), 0)
         out = torch.empty(2, dtype=torch.float32, device="cuda")
-        ws = torch.empty(self.L.sol_grad_clip_workspace_bytes(len(grads)), dtype=torch.uint8, device="cuda")
-        norm, coef = out[:1], out[1:]
-        self._check(self.L.sol_grad_clip(self.handle, arr, len(grads), max_norm, eps, int(bool(scale)), _ptr(norm), _ptr(coef), _ptr(ws),
-                                         ws.numel(), _stream(stream)))
+        need = self.L.sol_grad_clip_workspace_bytes(n)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        at = out.data_ptr()
+        self._check(self.L.sol_grad_clip(self.handle, words, n, max_norm, eps, int(bool(scale)), at, at + 4, ws.data_ptr(), need,
+                                         _stream(stream)))
         _used_on(stream, ws, out)
-        return norm, coef
+        return out[:1], out[1:]
 
     def adamw_step(self, params, grads, exp_avg, exp_avg_sq, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, coef=None,
                    copies=None, stream=None):
         """AdamW on lists of contiguous tensors: params, exp_avg, exp_avg_sq float32, grads float32 or bfloat16, copies bfloat16
         (rounded parameters for the forward pass) or None. step: int32 [1] on the device, the number of this update from 1; lr: a
         number, or float32 [1] on the device; coef: grad_clip's coefficient, by which the gradients are multiplied on the way, or None."""
-        n = len(params)
-        _need(len(grads) == n and len(exp_avg) == n and len(exp_avg_sq) == n and (copies is None or len(copies) == n),
-              "the lists differ in length")
-        f32 = (torch.float32,)
-        _flat(params, f32, "params"), _flat(exp_avg, f32, "exp_avg"), _flat(exp_avg_sq, f32, "exp_avg_sq"), _flat(grads, _CODE, "grads")
-        if copies is not None:
-            _flat(copies, (torch.bfloat16,), "copies")
-        flat = []
-        for i in range(n):
-            p, g, c = params[i], grads[i], None if copies is None else copies[i]
-            size = p.numel()
-            _need(g.numel() == size and exp_avg[i].numel() == size and exp_avg_sq[i].numel() == size and
-                  (c is None or c.numel() == size), f"tensor {i}: parameter, gradient and states differ in size")
-            flat += (p.data_ptr(), exp_avg[i].data_ptr(), exp_avg_sq[i].data_ptr(), g.data_ptr(), 0 if c is None else c.data_ptr(), size,
-                     _CODE[g.dtype])
-        arr = (C.c_int64 * len(flat))(*flat)
+        words, n = _tensor_lists((params, exp_avg, exp_avg_sq, grads, copies), ("params", "exp_avg", "exp_avg_sq", "grads", "copies"),
+                                 (1, 1, 1, 3, 2), 3)
         here, by_tensor = torch.cuda.current_device(), isinstance(lr, torch.Tensor)
         step, coef, rate = (_at(t, dtype, (1,), here, what) for t, dtype, what in
                             ((step, torch.int32, "step"), (coef, torch.float32, "coef"), (lr if by_tensor else None, torch.float32, "lr")))
         cfg = AdamwCfg(0.0 if by_tensor else lr, betas[0], betas[1], eps, weight_decay)
-        self._check(self.L.sol_adamw_step(self.handle, arr, n, C.byref(cfg), step, rate, coef, _stream(stream)))
+        self._check(self.L.sol_adamw_step(self.handle, words, n, C.byref(cfg), step, rate, coef, _stream(stream)))
 
     def schedule_loglik(self, layers, head, tokens, targets, action_ids, nll_out=None, workspace=None, stream=None):
         """tokens/targets int32 [B][T]; action_ids int32 [B][G][T]. Returns nll float32 [B][G][T] (nats)."""
