@@ -238,6 +238,11 @@ def _at(t, dtype, shape, here, what):
     return t.data_ptr()
 
 
+def _like(t, logits, what):
+    if t.shape != logits.shape or t.dtype != logits.dtype or t.get_device() != logits.get_device():
+        raise ValueError(f"{what}: not like logits")
+
+
 def _row_step(t, what):
     """Elements from one row of t ([..][A], rows evenly spaced) to the next."""
     A = t.shape[-1]
@@ -520,42 +525,45 @@ class Sol:
         logits, rows with up to seven unused elements between them)."""
         here, dtype, shape = torch.cuda.current_device(), logits.dtype, logits.shape
         code = _CODE.get(dtype)
-        _need(code is not None and len(shape) == 4 and logits.get_device() == here,
-              "logits: [B][G][T][A] of float32 or bfloat16 on the current device is needed")
-        _need(mean in MEANS, "mean: 'steps' or 'schedules'")
-        _need(action_ids is not None, "action_ids are needed")
+        if code is None or len(shape) != 4 or logits.get_device() != here:
+            raise ValueError("logits: [B][G][T][A] of float32 or bfloat16 on the current device is needed")
+        if mean not in MEANS or action_ids is None:
+            raise ValueError("mean has to be 'steps' or 'schedules', and action_ids are needed")
         B, G, T, A = shape
-        steps = shape[:3]
-        ids = _at(action_ids, torch.int32, steps, here, "action_ids")
-        adv, old_logp, ref_logp = (_at(t, torch.float32, steps, here, what)
-                                   for t, what in ((adv, "adv"), (old_logp, "old_logp"), (ref_logp, "ref_logp")))
-        eff = _at(eff, torch.int32, (B, T), here, "eff")
-        for t, what in ((ref_logits, "ref_logits"), (grad_out, "grad_out")):
-            _need(t is None or (t.shape == shape and t.dtype == dtype and t.get_device() == here), f"{what}: not like logits")
-        ld = _row_step(logits, "logits")
-        if not want_grad:
+        steps, n, f32, i32 = shape[:3], B * G * T, torch.float32, torch.int32
+        ids, eff = _at(action_ids, i32, steps, here, "action_ids"), _at(eff, i32, (B, T), here, "eff")
+        adv, old_logp = _at(adv, f32, steps, here, "adv"), _at(old_logp, f32, steps, here, "old_logp")
+        ref_logp, ref, ref_ld, grad, grad_ld = _at(ref_logp, f32, steps, here, "ref_logp"), None, 0, None, 0
+        ld = A if logits.is_contiguous() else _row_step(logits, "logits")
+        if ref_logits is not None:
+            _like(ref_logits, logits, "ref_logits")
+            ref, ref_ld = ref_logits.data_ptr(), _row_step(ref_logits, "ref_logits")
+        if want_grad:
+            if grad_out is not None:
+                _like(grad_out, logits, "grad_out")
+                grad_ld = _row_step(grad_out, "grad_out")
+            else:
+                # rows of padded logits begin at other distances from 16 bytes than packed ones would: the gradient's as the logits' do
+                gap = (ld - A) % 8
+                grad_out, grad_ld = logits.new_empty((B, G, T, A + gap)), A + gap
+                if gap:
+                    grad_out = grad_out[..., :A]
+            grad = grad_out.data_ptr()
+        else:
             grad_out = None
-        elif grad_out is None:
-            # rows of padded logits begin at other distances from 16 bytes than packed ones would: the gradient's as the logits' do
-            gap = (ld - A) % 8
-            grad_out = logits.new_empty((B, G, T, A + gap))
-            if gap:
-                grad_out = grad_out[..., :A]
-        # one allocation: loss, stats, log-probabilities; one for the workspace
-        n = B * G * T
-        out = torch.empty(8 + n, dtype=torch.float32, device="cuda") if n else torch.zeros(8, dtype=torch.float32, device="cuda")
-        loss, stats, logp = out[:1], out[4:8], out[8:].view(steps)
+        # one allocation: loss, stats, log-probabilities and the workspace behind them
         need = self.L.sol_policy_workspace_bytes(B, G, T)
-        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-        cfg = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean])
-        at = out.data_ptr()
-        self._check(self.L.sol_policy_loss(
-            self.handle, logits.data_ptr(), code, ld, ids, adv, old_logp, ref_logp, None if ref_logits is None else ref_logits.data_ptr(),
-            0 if ref_logits is None else _row_step(ref_logits, "ref_logits"), eff, C.byref(cfg), B, G, T, A, at, at + 16, at + 32,
-            None if grad_out is None else grad_out.data_ptr(), 0 if grad_out is None else _row_step(grad_out, "grad_out"), ws.data_ptr(), need,
-            _stream(stream)))
-        _used_on(stream, ws, out, grad_out)
-        return {"loss": loss, "stats": stats, "logp": logp, "grad": grad_out}
+        room = torch.empty if n else torch.zeros
+        out = room(8 + n + need // 4 + 1, dtype=f32, device="cuda")
+        loss, _, stats, logp, _ = out.split((1, 3, 4, n, need // 4 + 1))
+        cfg, at = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean]), out.data_ptr()
+        rc = self.L.sol_policy_loss(self.handle, logits.data_ptr(), code, ld, ids, adv, old_logp, ref_logp, ref, ref_ld, eff, C.byref(cfg), B, G,
+                                    T, A, at, at + 16, at + 32, grad, grad_ld, at + 32 + 4 * n, need, _stream(stream))
+        if rc:
+            self._check(rc)
+        if stream is not None:
+            _used_on(stream, out, grad_out)
+        return {"loss": loss, "stats": stats, "logp": logp.view(steps), "grad": grad_out}
 
     def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
         """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
