@@ -949,6 +949,9 @@ static int launched(sol_ctx *ctx)
     return e == hipSuccess ? SOL_OK : fail(ctx, SOL_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
 }
 
+// These workspaces may begin anywhere: the sizes hold 256 bytes to spare
+static void *aligned(void *p) { return (void *)(((uintptr_t)p + 255) & ~(uintptr_t)255); }
+
 struct Range { uintptr_t from, to; };                          // bytes [from, to)
 static Range range_of(const void *p, uint64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + bytes}; }
 static bool meet(const Range &a, const Range &b) { return a.from < b.to && b.from < a.to; }
@@ -977,6 +980,7 @@ static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, 
                        void *grad_out, int64_t grad_ld, void *workspace, size_t ws_bytes, void *stream)
 {
     if (B < 0 || G < 0 || T < 0 || A <= 0) return fail(ctx, SOL_ERR_INVALID_ARG, "negative size, or no action");
+    if (A > 1 << 30) return fail(ctx, SOL_ERR_UNSUPPORTED, "more than 2^30 actions");
     if (!pc || !loss_out) return fail(ctx, SOL_ERR_INVALID_ARG, "cfg or loss_out is NULL");
     auto weight = [](double v) { return v >= 0.0 && v < INFINITY; };
     if (!(pc->clip_low >= 0.0 && pc->clip_low <= 1.0) || !(pc->clip_high >= 0.0) || !weight(pc->kl_coef) || !weight(pc->entropy_coef) ||
@@ -1004,7 +1008,6 @@ static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, 
     const size_t need = sol_policy_workspace_bytes(B, G, T);
     if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
     if (const int rc = on_device(ctx)) return rc;
-    Carver c(workspace);
     PolicyArgs q{};
     q.logits = logits; q.ref_logits = ref_logits; q.grad = grad_out;
     q.ld = ld; q.ref_ld = ref_ld; q.grad_ld = grad_ld;
@@ -1012,7 +1015,7 @@ static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, 
     q.loss = loss_out; q.stats = stats_out; q.logp = logp_out; q.flags = ctx->d_flags;
     q.dtype = dtype; q.B = B; q.G = G; q.T = T; q.A = A;
     launch_policy_loss(q, PolicyCfg{pc->clip_low, pc->clip_high, pc->kl_coef, pc->entropy_coef, pc->temperature, pc->scale, pc->mean == SOL_MEAN_SCHEDULES},
-                       c.take(policy_scratch_bytes(B)), (hipStream_t)stream);
+                       aligned(workspace), (hipStream_t)stream);
     return launched(ctx);
 }
 
@@ -1053,9 +1056,7 @@ static int grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double 
     const size_t need = sol_grad_clip_workspace_bytes(n_tensors);
     if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
     if (const int rc = on_device(ctx)) return rc;
-    Carver c(workspace);
-    launch_grad_clip(items.data(), n_tensors, max_norm, eps, scale_grads != 0, norm_out, coef_out, c.take(clip_scratch_bytes(n_tensors)),
-                     (hipStream_t)stream);
+    launch_grad_clip(items.data(), n_tensors, max_norm, eps, scale_grads != 0, norm_out, coef_out, aligned(workspace), (hipStream_t)stream);
     return launched(ctx);
 }
 

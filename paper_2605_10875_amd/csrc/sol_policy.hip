@@ -62,18 +62,20 @@ template <int BLOCK> __device__ __forceinline__ void policy_count(const PolicyAr
 }
 
 __global__ void __launch_bounds__(PL_BLOCK)
-k_policy_count(const int32_t *__restrict__ eff, int T, int32_t *__restrict__ n)
+k_policy_count(const int32_t *__restrict__ eff, int B, int T, int32_t *__restrict__ n)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.x;
     __shared__ int red[PL_BLOCK / 64];
-    int c = 0;
-    for (int t = threadIdx.x; t < T; t += PL_BLOCK) c += eff[(int64_t)b * T + t] != 0;
-    c = wave_sum_i(c);
-    if (lane == 0) red[threadIdx.x >> 6] = c;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < PL_BLOCK / 64; ++i) c += red[i];
-        n[b] = c;
+    for (int b = blockIdx.x; b < B; b += gridDim.x) {
+        int c = 0;
+        for (int t = threadIdx.x; t < T; t += PL_BLOCK) c += eff[(int64_t)b * T + t] != 0;
+        c = wave_sum_i(c);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 1; i < PL_BLOCK / 64; ++i) c += red[i];
+            n[b] = c;
+        }
+        __syncthreads();
     }
 }
 __global__ void __launch_bounds__(PL_BLOCK)
@@ -225,6 +227,14 @@ template <class T> __device__ __forceinline__ void policy_put(T *d, const float 
 #pragma unroll
         for (int i = 0; i < V; ++i) if ((unsigned)(j + i) < (unsigned)A) st(d + j + i, f[i]);
     }
+}
+
+// a row of zeros
+template <class T> __device__ __forceinline__ void policy_clear(T *d, int A, int lane, int lanes)
+{
+    constexpr int V = Vec16<T>::N;
+    const float zero[V] = {};
+    for (int64_t j = (int64_t)lane * V - policy_mis(d); j < A; j += lanes * V) policy_put(d, zero, (int)j, A, true);
 }
 
 // ---- sums over the LANES lanes of a row: inside a wave, or over the waves of the workgroup ---------------------------
@@ -405,25 +415,34 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     using P = PolicyPiece<T, EXACT, false>;
     constexpr int V = P::V, BLOCK = LANES > PL_BLOCK ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
     __shared__ float s_max[2][16], s_sum[5][16];
-    __shared__ double s_part[BLOCK / 64][4];
+    __shared__ double s_part[ROWS][4];                              // a group's share of the means, its first lane's alone
     __shared__ PolicyShares few;
     if (q.eff && !w_in) policy_count<BLOCK>(q, few);
     const int tid = threadIdx.x, lane = tid % LANES, A = q.A;
+    double *const sum = s_part[tid / LANES];
+    if (lane == 0) sum[0] = sum[1] = sum[2] = sum[3] = 0.0;
     const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T, used = (q.pieces + LANES - 1) / LANES;     // pieces per lane
-    double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < rows; first += (int64_t)gridDim.x * ROWS) {
         const int64_t at = first + tid / LANES;
         const bool there = at < rows;                               // (the same for all lanes of a row, as live is)
         const int row = (int)(there ? at : rows - 1);
         const double w = there ? policy_weight(q, row, w_all, w_in, few) : 0.0;
         const bool live = w != 0.0;
+        if (LANES >= 64 && !live) {                                 // the whole row's lanes: nothing to read or to compute
+            if (there && lane == 0 && q.logp) q.logp[row] = 0.f;
+            if (there && q.grad) policy_clear((T *)q.grad + (int64_t)row * q.grad_ld, A, lane, LANES);
+            continue;
+        }
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
         const bool same = EXACT && policy_mis(y) == mis;
         uint4 rx[CH], ry[EXACT ? CH : 1];
         auto pieces = [&](auto f) {                                 // f(piece, its first element), all of them in registers
-            static_for<CH>([&](auto c) { if (c < used) f(c, ((int)c * LANES + lane) * V - mis); });
+            static_for<CH>([&](auto c) {
+                if (c < used) f(c, ((int)c * LANES + lane) * V - mis);
+                if (CH * (EXACT ? 2 : 1) > 8) __builtin_amdgcn_sched_barrier(0);       // (not all pieces' elements at once)
+            });
         };
         pieces([&](auto c, int j) {
             const bool whole = live && j >= 0 && j + V <= A;
@@ -441,7 +460,7 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         pieces([&](auto c, int j) { P::max(rx[c], ry[EXACT ? (int)c : 0], r.a - j, m, s[4]); });
         reduce_some<LANES, EXACT, 2>(m, OpMaxF(), s_max);
         const float top = m[0];
-        const bool far = policy_is_far(m[0], k), far_ref = EXACT && policy_is_far(m[1], k);
+        const bool far = live && policy_is_far(m[0], k), far_ref = EXACT && live && policy_is_far(m[1], k);
         if (__any(far || far_ref)) {
             pieces([&](auto c, int) {
                 if (far) rx[c] = policy_centred<T>(rx[c], m[0]);
@@ -457,7 +476,7 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
                                   q.ref_logp != nullptr, EXACT);
         if (s[0] != s[0]) z.c = NAN;                                // (no distribution: no element's 2^t is 0)
         const bool dead = !live || s[0] == 0.f;                     // not an effective step, or no action allowed
-        if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
+        if (dead) { c = PolicyCoef{}; c.logp = live ? -INFINITY : 0.f; }
         if (there && lane == 0) {
             if (q.logp) q.logp[row] = c.logp;
             sum[0] += w * (double)c.pg;
@@ -475,17 +494,11 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             });
         }
     }
-    const int wave = tid >> 6;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        sum[i] = lanes_sum_f64(sum[i]);
-        if ((tid & 63) == 0) s_part[wave][i] = sum[i];
-    }
     __syncthreads();
     if (tid < 4) {
         double v = 0.0;
-#pragma unroll
-        for (int i = 0; i < BLOCK / 64; ++i) v += s_part[i][tid];
+#pragma unroll 4
+        for (int i = 0; i < ROWS; ++i) v += s_part[i][tid];
         partial[4 * (int64_t)blockIdx.x + tid] = v;
     }
 }
@@ -505,7 +518,8 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     const int tid = threadIdx.x, A = q.A;
     const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T, used = (q.pieces + BLOCK - 1) / BLOCK;
-    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    __shared__ double sum[4];                                       // the first lane's alone
+    if (tid == 0) sum[0] = sum[1] = sum[2] = sum[3] = 0.0;
     uint4 rx[CH], ry[EXACT ? CH : 1];
     const T *x = nullptr, *y = nullptr;                             // the row that is being loaded
     int mis = 0;
@@ -534,6 +548,8 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         const int mis_row = mis;
         PolicyRow r{};
         if (live_row) r = policy_inputs(q, (int)row, w_row, tid == 0);
+        // A row that does not count is -inf throughout and takes the same way: a branch around it would make every load that is
+        // under way wait at its end (313 -> 412 us for 2664 rows of 128256 bf16 logits).
         PolicyRunning<EXACT, false> u(k);
         float xa = 0.f, top;
         for (bool centred = false;; centred = true) {               // twice where the maximum is far from 0
@@ -555,7 +571,7 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             float n[2] = {u.m[0], u.m[1]};
             reduce_some<BLOCK, EXACT, 2>(n, OpMaxF(), s_max);
             if (!centred) top = n[0];
-            const bool far = policy_is_far(n[0], k), far_ref = EXACT && policy_is_far(n[1], k);
+            const bool far = live_row && policy_is_far(n[0], k), far_ref = EXACT && live_row && policy_is_far(n[1], k);
             if (centred || !(far || far_ref)) { u.turn(n); break; }
             static_for<CH>([&](auto i) {
                 if (i < used) {
@@ -570,8 +586,9 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         reduce_some<BLOCK, EXACT, 5>(u.s, OpAddF(), s_sum);
         PolicyCoef c = policy_row(pc, r, PolicySums{u.s[0], u.s[2], u.s[1], u.s[3], u.s[4]}, top, policy_t<false>(u.m[0], u.z),
                                   q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
-        if (u.s[0] != u.s[0]) u.z.c = NAN;
-        if (!live_row || u.s[0] == 0.f) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live_row ? -INFINITY : 0.f; }
+        PolicyScale z = u.z;
+        if (u.s[0] != u.s[0]) z.c = NAN;
+        if (!live_row || u.s[0] == 0.f) { c = PolicyCoef{}; c.logp = live_row ? -INFINITY : 0.f; }
         if (tid == 0) {
             if (q.logp) q.logp[row] = c.logp;
             sum[0] += w_row * (double)c.pg;
@@ -587,7 +604,7 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
                 if (d) {
                     const int j = ((int)i * BLOCK + tid) * V - mis_row;
                     float o[V];
-                    P::grad(rx[i], ry[EXACT ? (int)i : 0], u.z, u.zr, c, r.a - j, o);
+                    P::grad(rx[i], ry[EXACT ? (int)i : 0], z, u.zr, c, r.a - j, o);
                     if (j < A) policy_put(d, o, j, A, vec);
                 }
                 request(i);
@@ -596,7 +613,6 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         });
     }
     if (tid == 0)
-#pragma unroll
         for (int i = 0; i < 4; ++i) partial[4 * (int64_t)blockIdx.x + i] = sum[i];
 }
 
@@ -614,37 +630,40 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
     const int tid = threadIdx.x, A = q.A;
     const float k = (float)pc.inv_temp * PL_LOG2E;
     const int rows = q.B * q.G * q.T;
-    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    __shared__ double sum[4];                                       // the first lane's alone
+    if (tid == 0) sum[0] = sum[1] = sum[2] = sum[3] = 0.0;
     for (int row = blockIdx.x; row < rows; row += gridDim.x) {
         const double w = uniform(policy_weight(q, row, w_all, w_in, few));
         T *const d = q.grad ? (T *)q.grad + (int64_t)row * q.grad_ld : nullptr;
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
         const bool same = EXACT && policy_mis(y) == mis, vec = d && policy_mis(d) == mis;
-        const bool live = w != 0.0;
-        PolicyRow r{};
-        if (live) r = policy_inputs(q, row, w, tid == 0);
+        if (w == 0.0) {
+            if (tid == 0 && q.logp) q.logp[row] = 0.f;
+            if (d) policy_clear(d, A, tid, BLOCK);
+            continue;
+        }
+        const PolicyRow r = policy_inputs(q, row, w, tid == 0);
         auto piece = [&](const T *v, bool aligned, int j) {
             return aligned && j >= 0 && j + V <= A ? *(const uint4 *)(v + j) : j < A ? policy_edge(v, j, A) : policy_none<T>();
         };
         PolicyRunning<EXACT, true> u(k);
         float xa = 0.f;
-        if (live)
-            for (int j0 = tid * V - mis; j0 < A; j0 += CH * BLOCK * V) {
-                uint4 rx[CH], ry[CH];
+        for (int j0 = tid * V - mis; j0 < A; j0 += CH * BLOCK * V) {
+            uint4 rx[CH], ry[CH];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    const int j = j0 + c * BLOCK * V;
-                    rx[c] = piece(x, true, j);
-                    if (EXACT) ry[c] = piece(y, same, j);
-                }
-                float n[2] = {u.m[0], u.m[1]};
-#pragma unroll
-                for (int c = 0; c < CH; ++c) P::max(rx[c], ry[c], r.a - (j0 + c * BLOCK * V), n, xa);
-                u.turn(n);
-#pragma unroll
-                for (int c = 0; c < CH; ++c) P::sums(rx[c], ry[c], u.z, u.zr, u.s);
+            for (int c = 0; c < CH; ++c) {
+                const int j = j0 + c * BLOCK * V;
+                rx[c] = piece(x, true, j);
+                if (EXACT) ry[c] = piece(y, same, j);
             }
+            float n[2] = {u.m[0], u.m[1]};
+#pragma unroll
+            for (int c = 0; c < CH; ++c) P::max(rx[c], ry[c], r.a - (j0 + c * BLOCK * V), n, xa);
+            u.turn(n);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) P::sums(rx[c], ry[c], u.z, u.zr, u.s);
+        }
         float top[2] = {u.m[0], u.m[1]};
         reduce_some<BLOCK, EXACT, 2>(top, OpMaxF(), s_max);
         u.turn(top);
@@ -652,8 +671,8 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
         reduce_some<BLOCK, EXACT, 5>(u.s, OpAddF(), s_sum);
         PolicyCoef c = policy_row(pc, r, PolicySums{u.s[0], u.s[2], u.s[1], u.s[3], u.s[4]}, u.m[0], 0.f, q.old_logp != nullptr, q.ref_logp != nullptr, EXACT);
         if (u.s[0] != u.s[0]) u.z.c = NAN;
-        const bool dead = !live || u.s[0] == 0.f;
-        if (dead) { c.alpha = c.gamma = c.kappa = c.hot = 0.f; c.pg = c.kl = c.ent = c.clipped = 0.f; c.logp = live ? -INFINITY : 0.f; }
+        const bool dead = u.s[0] == 0.f;                            // no action allowed
+        if (dead) { c = PolicyCoef{}; c.logp = -INFINITY; }
         if (tid == 0) {
             if (q.logp) q.logp[row] = c.logp;
             sum[0] += w * (double)c.pg;
@@ -680,7 +699,6 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
             }
     }
     if (tid == 0)
-#pragma unroll
         for (int i = 0; i < 4; ++i) partial[4 * (int64_t)blockIdx.x + i] = sum[i];
 }
 
@@ -710,7 +728,16 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
     }
 }
 
-// The row's kernel by its number of 16-byte pieces.
+// The row's kernel by its number of 16-byte pieces. Rows of up to 32 KB (16 with a reference) stay in the registers of as few lanes as
+// hold them, so that many rows are under way per CU and few lanes repeat a row's scalars; longer ones fill the registers of a CU by
+// one or two, and load ahead (k_policy_ring); what does not fit is read twice. Measured, 200 M logits (bytes read and written / time, of
+// 5.06 TB/s that a copy of 1 GiB reaches):
+//   4096 bf16 logits: 64 lanes x 8 pieces 4.8 TB/s, 256 x 4 (two pieces each, two barriers per row) 3.6
+//   32768 bf16: 512 x 8 4.7, two sweeps 3.7;  65536 bf16: ring of 512 4.7, one workgroup of 1024 without loading ahead 3.8, two sweeps 3.7
+//   128256 bf16: ring of 1024 4.0 (4.4 where rows fill the CUs evenly), not loading ahead 3.2, two sweeps 3.6
+//   65536 fp32: ring 4.5, two sweeps 4.1;  32768 fp32 with a reference: 4.7 from the ring, 3.3 by two sweeps
+// bf16 with a reference is bound by its arithmetic (two exponentials, 35 instructions per pair): from 32 KB on two sweeps by four
+// workgroups per CU reach 3.7-3.9 TB/s, the ring, which spills there, 2.9.
 template <class T, bool EXACT>
 static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)
 {
@@ -722,27 +749,35 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
         grid = (int)(n < PL_GRID ? n : PL_GRID);
         hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
     };
-    auto ring = [&](auto kern, int block) {                         // as many workgroups as fit the chip: 16 waves per CU
-        const int cus = device_cus(), fit = (cus > 0 ? cus : 256) * (1024 / block);
-        grid = rows < fit ? rows : fit;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
+    auto held = [&](auto lanes, auto ch) {
+        constexpr int L = decltype(lanes)::value, C = decltype(ch)::value, BLOCK = L > PL_BLOCK ? L : PL_BLOCK;
+        go(k_policy_held<T, EXACT, L, C>, BLOCK, BLOCK / L);
     };
-#define HELD(L, C) go(k_policy_held<T, EXACT, L, C>, L > PL_BLOCK ? L : PL_BLOCK, (L > PL_BLOCK ? L : PL_BLOCK) / L)
-    if (pieces <= 8) HELD(8, 1);
-    else if (pieces <= 16) HELD(8, 2);
-    else if (pieces <= 32) HELD(8, 4);
-    else if (pieces <= 64) HELD(16, 4);
-    else if (pieces <= 128) HELD(32, 4);
-    else if (pieces <= 256) HELD(64, 4);
-    else if (pieces <= 512) HELD(64, 8);
-    else if (pieces <= 1024) HELD(256, 4);
-    else if (pieces <= 2048) HELD(256, 8);
-    else if (pieces <= 4096) HELD(512, 8);
-    else if (!EXACT && pieces <= 8192) ring(k_policy_ring<T, EXACT, (EXACT ? 1024 : 512), (EXACT ? 8 : 16)>, 512);
-    else if (HEAVY) go(k_policy_stream<T, EXACT, (HEAVY ? 512 : 1024), (HEAVY ? 4 : 2)>, 512, 1);
-    else if (pieces <= (EXACT ? 8192 : 16384)) ring(k_policy_ring<T, EXACT, 1024, (EXACT ? 8 : 16)>, 1024);
-    else go(k_policy_stream<T, EXACT, (HEAVY ? 512 : 1024), (HEAVY ? 4 : 2)>, 1024, 1);
-#undef HELD
+    auto ring = [&](auto block, auto ch) {                          // as many workgroups as fit the chip: 16 waves per CU
+        constexpr int BLOCK = decltype(block)::value;
+        const int cus = device_cus(), fit = (cus > 0 ? cus : 256) * (1024 / BLOCK);
+        grid = rows < fit ? rows : fit < PL_GRID ? fit : PL_GRID;
+        hipLaunchKernelGGL((k_policy_ring<T, EXACT, BLOCK, decltype(ch)::value>), dim3(grid), dim3(BLOCK), 0, st, q, pc, w_all, w, partial);
+    };
+#define N(n) std::integral_constant<int, n>{}
+    if (pieces <= 8) held(N(8), N(1));
+    else if (pieces <= 16) held(N(8), N(2));
+    else if (pieces <= 32) held(N(8), N(4));
+    else if (pieces <= 64) held(N(16), N(4));
+    else if (pieces <= 128) held(N(32), N(4));
+    else if (pieces <= 256) held(N(64), N(4));
+    else if (pieces <= 512) held(N(64), N(8));
+    else if (pieces <= 1024) held(N(256), N(4));
+    else if (pieces <= 2048) held(N(256), N(8));
+    else if constexpr (HEAVY) go(k_policy_stream<T, EXACT, 512, 4>, 512, 1);
+    else if (pieces <= 4096) held(N(512), N(8));
+    else if constexpr (EXACT) {
+        if (pieces <= 8192) ring(N(1024), N(8));
+        else go(k_policy_stream<T, EXACT, 1024, 2>, 1024, 1);
+    } else if (pieces <= 8192) ring(N(512), N(16));
+    else if (pieces <= 16384) ring(N(1024), N(16));
+    else go(k_policy_stream<T, EXACT, 1024, 2>, 1024, 1);
+#undef N
     return grid;
 }
 
@@ -764,7 +799,7 @@ void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStre
     const double w_all = 1.0 / ((double)q.B * q.G * q.T);           // every step counts: both means are one
     const bool few = (int64_t)q.B * q.T <= PL_FEW && q.B <= PL_INPUTS;
     if (q.eff && !few) {
-        hipLaunchKernelGGL(k_policy_count, dim3(q.B), dim3(PL_BLOCK), 0, st, q.eff, q.T, n);
+        hipLaunchKernelGGL(k_policy_count, dim3(q.B < PL_GRID ? q.B : PL_GRID), dim3(PL_BLOCK), 0, st, q.eff, q.B, q.T, n);
         hipLaunchKernelGGL(k_policy_weights, dim3(1), dim3(PL_BLOCK), 0, st, n, q.B, q.G, g.by_schedule, w);
     } else w = nullptr;
     const int rows = q.B * q.G * q.T;

@@ -135,9 +135,9 @@ k_grad_norm(const double *__restrict__ partial, int64_t n, double max_norm, doub
     for (int64_t i = threadIdx.x; i < n; i += 1024) s += partial[i];
     s = sqrt(up_block_sum<1024>(s, red));
     if (threadIdx.x == 0) {
-        *norm = (float)s;
         const double c = max_norm / (s + eps);
-        *coef = !(s < INFINITY) ? NAN : c < 1.0 ? (float)c : 1.f;
+        *norm = (float)s;
+        *coef = !((float)s < INFINITY) ? NAN : c < 1.0 ? (float)c : 1.f;
     }
 }
 
