@@ -261,6 +261,39 @@ def test_the_loss_by_differences(ctx, A):
     assert abs((up - down) / (2 * h) - along) < 8 * h * h / 6 * 3 + 2.0 ** -23 * (abs(up) + 1) / h * 2
 
 
+@pytest.mark.parametrize("A,dtype,kl,T", [(64, torch.bfloat16, "logits", 1 << 17), (9, torch.float32, "none", 1 << 17), (700, torch.float32, "logp", 16384),
+                                          (4001, torch.float32, "logits", 4096), (9001, torch.float32, "none", 4096),
+                                          (16400, torch.float32, "none", 2048), (33001, torch.float32, "logp", 1024),
+                                          (33001, torch.bfloat16, "none", 2048), (70001, torch.bfloat16, "none", 1024),
+                                          (20001, torch.float32, "logits", 1024), (40001, torch.bfloat16, "logits", 4096),
+                                          (70001, torch.float32, "none", 4096)])
+@pytest.mark.parametrize("skip", [False, True])
+def test_a_row_does_not_depend_on_its_place(ctx, A, dtype, kl, T, skip):
+    """More rows than workgroups, every second one not effective where `skip`, against the same rows in eight calls: the shares are powers
+    of two, so that scale * share is the same number."""
+    gen = torch.Generator(device="cuda").manual_seed(A)
+    x = torch.randn((1, 1, T, A), generator=gen, device="cuda").to(dtype)
+    ref = {"none": {}, "logp": {"ref_logp": torch.full((1, 1, T), -8.0, device="cuda"), "kl_coef": 0.1},
+           "logits": {"ref_logits": (x.float() + 0.3).to(dtype).flip(-1).contiguous(), "kl_coef": 0.1}}[kl]
+    ids = torch.randint(0, A, (1, 1, T), generator=gen, device="cuda").int()
+    steps = {"adv": torch.randn((1, 1, T), generator=gen, device="cuda"), "old_logp": torch.full((1, 1, T), -9.0, device="cuda")}
+    eff = torch.ones((1, T), dtype=torch.int32, device="cuda")
+    if skip:
+        eff[:, ::2] = 0
+    got = ctx.policy_loss(x, ids, eff=eff, scale=float(T), entropy_coef=0.05, **steps, **ref)
+    n, loss = T // 8, 0.0
+    for k in range(8):
+        part = slice(k * n, (k + 1) * n)
+        cut = {k2: (v if isinstance(v, float) else v[:, :, part].contiguous()) for k2, v in {**steps, **ref}.items()}
+        one = ctx.policy_loss(x[:, :, part].contiguous(), ids[:, :, part].contiguous(), eff=eff[:, part].contiguous(), scale=float(n), entropy_coef=0.05, **cut)
+        assert torch.equal(one["grad"], got["grad"][:, :, part]) and torch.equal(one["logp"], got["logp"][:, :, part])
+        loss += float(one["loss"])
+        if skip:
+            assert not one["grad"][:, :, ::2].any() and not one["logp"][:, :, ::2].any() and one["grad"][:, :, 1::2].any()
+    assert abs(float(got["loss"]) - loss) <= 2.0 ** -23 * (abs(loss) + 8 * T)       # each loss rounded once
+    assert ctx.device_status() == sol.OK
+
+
 def test_same_bits_again_on_another_stream_and_replayed(ctx):
     cases = [_case(2, 3, 7, A, dt, kl=kl, ragged=True, seed=11) for A, dt, kl in ((80, torch.float32, "logp"), (5000, torch.bfloat16, "logits"),
                                                                                  (140001, torch.float32, "none"))]
