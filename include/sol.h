@@ -295,15 +295,18 @@ int sol_reward_advantages(sol_ctx *ctx, const float *nll, const int32_t *action_
  * device: loss_out float [1]; stats_out float [4], the means of pg, KL, H and of the share of clipped rows, or NULL; logp_out float
  * [B][G][T], the actions' log-probabilities (the next update's old_logp), or NULL; grad_out rows of A elements of dtype, grad_ld
  * apart, or NULL (loss alone). grad_out may be logits itself with grad_ld == ld; any other overlap with the logits is refused, and
- * elements between the rows are left as they are. Sums are held in 32 bits per row and in 64 over the rows; a row's gradient is rounded
- * once. Workspace: sol_policy_workspace_bytes(B, G, T). B * G * T == 0 is a no-op (loss_out is left as it is); at most 2^31 - 1 rows. */
+ * elements between the rows are left as they are. Where the reference forbids an action that the policy allows, KL is infinite and the
+ * row's gradient is not finite. A row's elements are summed in 32 bits, its log-probability, the test of the ratio's bounds and the sums
+ * over the rows are in 64; a gradient is rounded once. The order of a row's sums depends on A, on the number of elements that the row
+ * begins behind a 16-byte boundary and on nothing else. Workspace: sol_policy_workspace_bytes(B, G, T), device memory of any alignment.
+ * B * G * T == 0 is a no-op (loss_out is left as it is); at most 2^31 - 1 rows of 2^30 actions. */
 #define SOL_MEAN_STEPS 0
 #define SOL_MEAN_SCHEDULES 1
 typedef struct {
     double  clip_low, clip_high;              /* the ratio's bounds are 1 - clip_low and 1 + clip_high; clip_low in [0, 1], clip_high >= 0 */
-    double  kl_coef, entropy_coef;            /* >= 0; kl_coef > 0 needs a reference */
-    double  temperature;                      /* > 0 */
-    double  scale;                            /* factor of loss and gradient (e.g. 1 / accumulated batches) */
+    double  kl_coef, entropy_coef;            /* in [0, 1e30]; kl_coef > 0 needs a reference */
+    double  temperature;                      /* in [2^-20, 2^20] */
+    double  scale;                            /* factor of loss and gradient (e.g. 1 / accumulated batches), in [-1e30, 1e30] */
     int32_t mean;                             /* SOL_MEAN_STEPS or SOL_MEAN_SCHEDULES */
 } sol_policy_cfg;
 size_t sol_policy_workspace_bytes(int B, int G, int T);
@@ -315,10 +318,11 @@ int sol_policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, con
 /* Global norm of many gradients, and clipping:
  *   norm_out[0] = sqrt(sum over all elements of all tensors of g^2),  coef_out[0] = min(1, max_norm / (norm + eps)),
  * and, with scale_grads != 0, every gradient is multiplied by coef in place (rounded to its type; untouched where coef is 1). The squares
- * are summed in 64 bits. If the norm is not finite, coef_out is NaN and the gradients are left as they are. grads: HOST array of
- * n_tensors entries (read during the call only, captured by value under graph capture): device data, elements, sol_dtype; contiguous,
- * aligned to their elements, n == 0 allowed; overlapping ones are refused where they are scaled. max_norm > 0 (INFINITY: measure
- * only). norm_out, coef_out: device float [1]. Workspace: sol_grad_clip_workspace_bytes(n_tensors). */
+ * are summed in 64 bits, in an order that depends on the list's sizes, types and alignments alone. If norm_out is not finite, coef_out is
+ * NaN and the gradients are left as they are. grads: HOST array of n_tensors entries (read during the call only, captured by value under
+ * graph capture): device data, elements, sol_dtype; contiguous, aligned to their elements, n == 0 allowed, 2^37 elements in all at most;
+ * overlapping ones are refused where they are scaled. max_norm > 0 (INFINITY: measure only). norm_out, coef_out: device float [1].
+ * Workspace: sol_grad_clip_workspace_bytes(n_tensors), device memory of any alignment. */
 typedef struct { void *data; int64_t n; int32_t dtype; int32_t reserved; } sol_grad;
 size_t sol_grad_clip_workspace_bytes(int n_tensors);
 int sol_grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double max_norm, double eps, int scale_grads, float *norm_out,

@@ -949,6 +949,8 @@ static int launched(sol_ctx *ctx)
     return e == hipSuccess ? SOL_OK : fail(ctx, SOL_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
 }
 
+static_assert(sizeof(sol_grad) == 24 && sizeof(sol_adamw_tensor) == 56 && sizeof(sol_policy_cfg) == 56 && sizeof(sol_adamw_cfg) == 40, "the binding's records");
+
 // These workspaces may begin anywhere: the sizes hold 256 bytes to spare
 static void *aligned(void *p) { return (void *)(((uintptr_t)p + 255) & ~(uintptr_t)255); }
 
@@ -982,10 +984,10 @@ static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, 
     if (B < 0 || G < 0 || T < 0 || A <= 0) return fail(ctx, SOL_ERR_INVALID_ARG, "negative size, or no action");
     if (A > 1 << 30) return fail(ctx, SOL_ERR_UNSUPPORTED, "more than 2^30 actions");
     if (!pc || !loss_out) return fail(ctx, SOL_ERR_INVALID_ARG, "cfg or loss_out is NULL");
-    auto weight = [](double v) { return v >= 0.0 && v < INFINITY; };
+    auto weight = [](double v) { return v >= 0.0 && v <= 1e30; };                      // (rows are computed in 32 bits)
     if (!(pc->clip_low >= 0.0 && pc->clip_low <= 1.0) || !(pc->clip_high >= 0.0) || !weight(pc->kl_coef) || !weight(pc->entropy_coef) ||
-        !(pc->temperature > 0.0 && pc->temperature < INFINITY) || !std::isfinite(pc->scale))
-        return fail(ctx, SOL_ERR_INVALID_ARG, "policy cfg: clip_low in [0, 1], clip_high >= 0, coefficients >= 0 and finite, temperature > 0, scale finite");
+        !(pc->temperature >= 0x1p-20 && pc->temperature <= 0x1p20) || !weight(std::fabs(pc->scale)))
+        return fail(ctx, SOL_ERR_INVALID_ARG, "policy cfg: clip_low in [0, 1], clip_high >= 0, coefficients in [0, 1e30], temperature in [2^-20, 2^20], scale in [-1e30, 1e30]");
     if (pc->mean != SOL_MEAN_STEPS && pc->mean != SOL_MEAN_SCHEDULES) return fail(ctx, SOL_ERR_INVALID_ARG, "policy cfg: unknown mean");
     if (dtype != SOL_F32 && dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, "dtype must be SOL_F32 or SOL_BF16");
     if (ref_logp && ref_logits) return fail(ctx, SOL_ERR_INVALID_ARG, "ref_logp and ref_logits exclude each other");
@@ -1040,6 +1042,7 @@ static int grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double 
     if (n_tensors < 0 || (n_tensors > 0 && !grads)) return fail(ctx, SOL_ERR_INVALID_ARG, "no list of gradients");
     if (!norm_out || !coef_out) return fail(ctx, SOL_ERR_INVALID_ARG, "norm_out or coef_out is NULL");
     if (!(max_norm > 0.0) || !(eps >= 0.0 && eps < INFINITY)) return fail(ctx, SOL_ERR_INVALID_ARG, "max_norm must be > 0, eps >= 0 and finite");
+    uint64_t total = 0;
     std::vector<GradItem> items((size_t)n_tensors);
     std::vector<Range> at;
     at.reserve((size_t)n_tensors);
@@ -1050,6 +1053,8 @@ static int grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double 
         if (g.dtype != SOL_F32 && g.dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": dtype must be SOL_F32 or SOL_BF16");
         if ((uintptr_t)g.data % esize(g.dtype)) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": not aligned to its elements");
         items[i] = GradItem{g.data, g.n, g.dtype};
+        total += g.n <= CLIP_MOST ? (uint64_t)g.n : CLIP_MOST + 1;
+        if (total > CLIP_MOST) return fail(ctx, SOL_ERR_UNSUPPORTED, "more than 2^37 elements");
         if (g.n) at.push_back(range_of(g.data, (uint64_t)g.n * esize(g.dtype)));
     }
     if (scale_grads && any_meet(at, at.size())) return fail(ctx, SOL_ERR_INVALID_ARG, "two gradients overlap");

@@ -258,6 +258,7 @@ void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStre
 struct GradItem { void *g; int64_t n; int dtype; };
 struct AdamItem { float *p, *m, *v; const void *g; void *copy; int64_t n; int dtype; };
 struct AdamCfg { double lr, beta1, beta2, eps, weight_decay; };
+constexpr uint64_t CLIP_MOST = (uint64_t)1 << 37;                  // elements of all gradients at most
 size_t clip_scratch_bytes(int count);
 void launch_grad_clip(const GradItem *items, int count, double max_norm, double eps, bool scale, float *norm, float *coef, void *scratch,
                       hipStream_t st);

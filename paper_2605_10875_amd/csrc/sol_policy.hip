@@ -702,14 +702,15 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
         for (int i = 0; i < 4; ++i) partial[4 * (int64_t)blockIdx.x + i] = sum[i];
 }
 
-// the workgroups' sums in a fixed order; out: policy term, KL, entropy, clipped share
-__global__ void __launch_bounds__(PL_BLOCK)
+// the workgroups' sums in a fixed order; stats: policy term, KL, entropy, clipped share
+constexpr int PL_FINISH = 1024;
+__global__ void __launch_bounds__(PL_FINISH)
 k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, float *__restrict__ loss, float *__restrict__ stats)
 {
-    __shared__ double red[PL_BLOCK / 64][4];
+    __shared__ double red[PL_FINISH / 64][4];
     double v[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += PL_BLOCK)
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n; i += PL_FINISH)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += partial[4 * i + e];
 #pragma unroll
@@ -720,7 +721,11 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]);
+        for (int e = 0; e < 4; ++e) {
+            v[e] = 0.0;
+#pragma unroll
+            for (int i = 0; i < PL_FINISH / 64; ++i) v[e] += red[i][e];
+        }
         *loss = (float)(pc.scale * (v[0] + pc.kl * v[1] - pc.ent * v[2]));
         if (stats)
 #pragma unroll
@@ -807,7 +812,7 @@ void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStre
                                                   : launch_rows<bf16_t, false>(q, pc, w_all, w, partial, rows, st))
                                   : (q.ref_logits ? launch_rows<float, true>(q, pc, w_all, w, partial, rows, st)
                                                   : launch_rows<float, false>(q, pc, w_all, w, partial, rows, st));
-    hipLaunchKernelGGL(k_policy_finish, dim3(1), dim3(PL_BLOCK), 0, st, partial, grid, pc, q.loss, q.stats);
+    hipLaunchKernelGGL(k_policy_finish, dim3(1), dim3(PL_FINISH), 0, st, partial, grid, pc, q.loss, q.stats);
 }
 
 }  // namespace sol

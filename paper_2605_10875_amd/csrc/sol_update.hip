@@ -251,9 +251,10 @@ static void in_parts(const Item *items, int count, Step step, Put put, F f)
     }
 }
 
-// partial sums of as many launches as `count` tensors can take: 240 places each, one launch more per type, and what tensors of over 2^31
-// elements take besides (fewer than 240 in any memory)
-size_t clip_scratch_bytes(int count) { return ((size_t)count / UP_CLIP + 4) * UP_PARTS * sizeof(double); }
+// Partial sums of as many launches as `count` tensors of CLIP_MOST elements in all can take: UP_CLIP places each, one launch more per type
+// (2), the 64 further places of tensors of over 2^31 elements (1), launches that end at UP_STEPS steps (2).
+size_t clip_scratch_bytes(int count) { return ((size_t)count / UP_CLIP + 5) * UP_PARTS * sizeof(double); }
+static_assert(CLIP_MOST / UP_LONGEST < UP_CLIP && CLIP_MOST / clip_step<float>() <= 3 * UP_STEPS, "launches of the norm");
 
 void launch_grad_clip(const GradItem *items, int count, double max_norm, double eps, bool scale, float *norm, float *coef, void *scratch,
                       hipStream_t st)

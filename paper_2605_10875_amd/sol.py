@@ -554,11 +554,11 @@ class Sol:
         # one allocation: loss, stats, log-probabilities and the workspace behind them
         need = self.L.sol_policy_workspace_bytes(B, G, T)
         room = torch.empty if n else torch.zeros
-        out = room(8 + n + need // 4 + 1, dtype=f32, device="cuda")
-        loss, _, stats, logp, _ = out.split((1, 3, 4, n, need // 4 + 1))
+        out = room(5 + n + need // 4 + 1, dtype=f32, device="cuda")
+        loss, stats, logp, _ = out.split_with_sizes((1, 4, n, need // 4 + 1))
         cfg, at = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean]), out.data_ptr()
         rc = self.L.sol_policy_loss(self.handle, logits.data_ptr(), code, ld, ids, adv, old_logp, ref_logp, ref, ref_ld, eff, C.byref(cfg), B, G,
-                                    T, A, at, at + 16, at + 32, grad, grad_ld, at + 32 + 4 * n, need, _stream(stream))
+                                    T, A, at, at + 4, at + 20, grad, grad_ld, at + 20 + 4 * n, need, _stream(stream))
         if rc:
             self._check(rc)
         if stream is not None:

@@ -324,6 +324,34 @@ def test_same_bits_again_on_another_stream_and_replayed(ctx):
             assert all(torch.equal(a[k], b[k]) for k in a), i
 
 
+def test_two_streams_at_once(ctx):
+    """The operators of a set keep nothing between calls: two of each under way at the same time give what they give alone."""
+    cases = [_case(4, 8, 64, A, dt, kl=kl, ragged=True, seed=20) for A, dt, kl in ((4001, torch.float32, "logits"), (33001, torch.bfloat16, "logp"))]
+    fixed = [(x, dev(ids), {k: v if not isinstance(v, np.ndarray) else dev(v) for k, v in kw.items()}) for x, ids, kw in cases]
+    grads = [[torch.randn(n, device="cuda") for n in (1 << 20, 333, 70001)] for _ in range(2)]
+    alone = [ctx.policy_loss(x, ids, **kw) for x, ids, kw in fixed]
+    norms = [[t.clone() for t in ctx.grad_clip(g, 1.0, scale=False)] for g in grads]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in fixed]
+    got = [[], []]
+    for _ in range(10):
+        for k, (x, ids, kw) in enumerate(fixed):
+            with torch.cuda.stream(streams[k]):
+                got[k].append((ctx.policy_loss(x, ids, **kw), ctx.grad_clip(grads[k], 1.0, scale=False)))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out, nc in got[k]:
+            assert all(torch.equal(out[n], alone[k][n]) for n in out)
+            assert torch.equal(nc[0], norms[k][0]) and torch.equal(nc[1], norms[k][1])
+
+
+@pytest.mark.parametrize("temperature", [2.0 ** -20, 1e-3, 50.0, 2.0 ** 20])
+@pytest.mark.parametrize("A", [9, 5000])
+def test_temperatures_at_the_ends(ctx, temperature, A):
+    x, ids, kw = _case(1, 2, 4, A, temperature=temperature, seed=21, spread=min(2.0, 2.0 * temperature))
+    _check(_run(ctx, x, ids, kw), _oracle(x, ids, kw), x, kw, _rel(x, kw))
+
+
 def test_refusals(ctx):
     x, ids, kw = _case(1, 2, 3, 8, kl="logp", seed=12)
 
@@ -334,7 +362,7 @@ def test_refusals(ctx):
         assert e.value.code == code, e.value
 
     for change in (dict(clip=(-0.1, 0.2)), dict(clip=(1.1, 0.2)), dict(clip=(0.2, -1.0)), dict(kl_coef=-1.0), dict(kl_coef=float("nan")),
-                   dict(entropy_coef=float("inf")), dict(temperature=0.0), dict(temperature=float("nan")), dict(scale=float("inf")),
+                   dict(entropy_coef=float("inf")), dict(entropy_coef=1e31), dict(temperature=1e-7), dict(temperature=0.0), dict(temperature=float("nan")), dict(scale=float("inf")),
                    dict(ref_logits=x.clone()), dict(ref_logp=None)):
         bad(sol.ERR_INVALID_ARG, **change)
     big = torch.zeros(3 * 6 * 8, device="cuda")

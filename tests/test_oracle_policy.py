@@ -55,7 +55,7 @@ def test_against_differentiation_by_torch(kl, temperature):
         loss = loss + 0.1 * (lp.exp() * (fin - lq.masked_fill(lq == -np.inf, 0.0))).sum(-1)
     loss = 0.5 * loss.mean()
     loss.backward()
-    assert abs(float(loss) - got["loss"]) < 1e-12
+    assert abs(float(loss.detach()) - got["loss"]) < 1e-12
     np.testing.assert_allclose(got["grad"], t.grad.numpy(), rtol=0, atol=1e-14)
 
 
