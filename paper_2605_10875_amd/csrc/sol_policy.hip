@@ -186,30 +186,56 @@ __device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const 
 }
 
 // ---- a row's elements in 16-byte pieces -------------------------------------------------------------------------
-// Piece i of a row covers elements V i - mis .. V i - mis + V - 1, mis being the row's distance from a 16-byte boundary in elements,
-// so that every piece inside the row is one aligned access whatever the row's length and start are. Elements outside are -inf.
+// Piece i of a row covers elements V i - mis .. V i - mis + V - 1, mis being the row's distance from a 16-byte boundary in elements: inside
+// the row every piece is one aligned access whatever the row's length and start are. The pieces that the row's ends cut are loaded
+// as the 16 bytes at that end, not aligned, and shifted into place once they are there (policy_cut); elements outside are -inf.
 template <class T> __device__ __forceinline__ int policy_mis(const T *x) { return (int)(((uintptr_t)x & 15) / sizeof(T)); }
 template <class T> __device__ __forceinline__ uint4 policy_none()
 {
     const uint32_t w = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
     return make_uint4(w, w, w, w);
 }
-template <class T> __device__ __forceinline__ uint4 policy_edge(const T *x, int j, int A)
+// the 16 bytes nearest to element j that lie in the row; element by element for rows that have fewer, which are not LONG
+template <bool LONG, class T> __device__ __forceinline__ uint4 policy_load(const T *x, int j, int A)
 {
-    uint32_t w[4];
     constexpr int V = Vec16<T>::N;
-    if (sizeof(T) == 4) {
+    uint4 r;
+    if (LONG || A >= V) {
+        const int at = j < 0 ? 0 : j > A - V ? A - V : j;
+        __builtin_memcpy(&r, x + at, 16);
+        return r;
+    }
+    uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) w[i] = (unsigned)(j + i) < (unsigned)A ? ((const uint32_t *)x)[j + i] : 0xFF800000u;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i += 2) {
-            const uint32_t lo = (unsigned)(j + i) < (unsigned)A ? ((const uint16_t *)x)[j + i] : 0xFF80u;
-            const uint32_t hi = (unsigned)(j + i + 1) < (unsigned)A ? ((const uint16_t *)x)[j + i + 1] : 0xFF80u;
-            w[i / 2] = lo | hi << 16;
+    for (int i = 0; i < 4; ++i) {
+        const int e = j + i * (V / 4);
+        if (sizeof(T) == 4) w[i] = (unsigned)e < (unsigned)A ? ((const uint32_t *)x)[e] : 0xFF800000u;
+        else {
+            const uint32_t lo = (unsigned)e < (unsigned)A ? ((const uint16_t *)x)[e] : 0xFF80u;
+            const uint32_t hi = (unsigned)(e + 1) < (unsigned)A ? ((const uint16_t *)x)[e + 1] : 0xFF80u;
+            w[i] = lo | hi << 16;
         }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// what policy_load(x, j, A) gave, as elements j .. j + V - 1: the four words moved by whole words, then by half of one
+template <bool LONG, class T> __device__ __forceinline__ uint4 policy_cut(uint4 r, int j, int A)
+{
+    constexpr int V = Vec16<T>::N, H = V / 4;                       // elements per word
+    if ((LONG || A >= V) && (j < 0 || j > A - V)) {
+        const uint32_t none = policy_none<T>().x;
+        const int by = j < 0 ? -j : j - (A - V);                    // elements, 0 < by < V
+        if (j < 0) {
+            if (by & 2 * H) r = make_uint4(none, none, r.x, r.y);
+            if (by & H) r = make_uint4(none, r.x, r.y, r.z);
+            if (H == 2 && (by & 1)) r = make_uint4(none >> 16 | r.x << 16, r.x >> 16 | r.y << 16, r.y >> 16 | r.z << 16, r.z >> 16 | r.w << 16);
+        } else {
+            if (by & 2 * H) r = make_uint4(r.z, r.w, none, none);
+            if (by & H) r = make_uint4(r.y, r.z, r.w, none);
+            if (H == 2 && (by & 1)) r = make_uint4(r.x >> 16 | r.y << 16, r.y >> 16 | r.z << 16, r.z >> 16 | r.w << 16, r.w >> 16 | none << 16);
+        }
+    }
+    return r;
 }
 template <class T> __device__ __forceinline__ void policy_unpack(uint4 raw, float *f)
 {
@@ -217,12 +243,14 @@ template <class T> __device__ __forceinline__ void policy_unpack(uint4 raw, floa
     v.raw = __builtin_bit_cast(decltype(v.raw), raw);
     v.unpack(f);
 }
-template <class T> __device__ __forceinline__ void policy_put(T *d, const float *f, int j, int A, bool vec)
+template <class T> __device__ __forceinline__ void policy_put(T *d, const float *f, int j, int A)
 {
     constexpr int V = Vec16<T>::N;
-    if (vec && j >= 0 && j + V <= A) {
-        if (sizeof(T) == 4) *(float4 *)(d + j) = make_float4(f[0], f[1], f[2], f[3]);
-        else *(uint4 *)(d + j) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4 % V], f[5 % V]), pack_bf16x2(f[6 % V], f[7 % V]));
+    if (j >= 0 && j + V <= A) {
+        uint4 r;
+        if (sizeof(T) == 4) r = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        else r = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4 % V], f[5 % V]), pack_bf16x2(f[6 % V], f[7 % V]));
+        __builtin_memcpy(d + j, &r, 16);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) if ((unsigned)(j + i) < (unsigned)A) st(d + j + i, f[i]);
@@ -234,7 +262,7 @@ template <class T> __device__ __forceinline__ void policy_clear(T *d, int A, int
 {
     constexpr int V = Vec16<T>::N;
     const float zero[V] = {};
-    for (int64_t j = (int64_t)lane * V - policy_mis(d); j < A; j += lanes * V) policy_put(d, zero, (int)j, A, true);
+    for (int64_t j = (int64_t)lane * V - policy_mis(d); j < A; j += lanes * V) policy_put(d, zero, (int)j, A);
 }
 
 // ---- sums over the LANES lanes of a row: inside a wave, or over the waves of the workgroup ---------------------------
@@ -436,7 +464,6 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         }
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
-        const bool same = EXACT && policy_mis(y) == mis;
         uint4 rx[CH], ry[EXACT ? CH : 1];
         auto pieces = [&](auto f) {                                 // f(piece, its first element), all of them in registers
             static_for<CH>([&](auto c) {
@@ -445,16 +472,17 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             });
         };
         pieces([&](auto c, int j) {
-            const bool whole = live && j >= 0 && j + V <= A;
-            rx[c] = whole ? *(const uint4 *)(x + j) : policy_none<T>();
-            if (EXACT) ry[EXACT ? (int)c : 0] = whole && same ? *(const uint4 *)(y + j) : policy_none<T>();
+            const bool in = live && j < A;
+            rx[c] = in ? policy_load<(LANES * CH > 16)>(x, j, A) : policy_none<T>();
+            if (EXACT) ry[EXACT ? (int)c : 0] = in ? policy_load<(LANES * CH > 16)>(y, j, A) : policy_none<T>();
         });
         PolicyRow r{};
         if (live) r = policy_inputs(q, row, w, lane == 0);
         pieces([&](auto c, int j) {
-            const bool part = live && j < A, cut = j < 0 || j + V > A;
-            if (part && cut) rx[c] = policy_edge(x, j, A);
-            if (EXACT && part && (cut || !same)) ry[EXACT ? (int)c : 0] = policy_edge(y, j, A);
+            if (live && j < A) {
+                rx[c] = policy_cut<(LANES * CH > 16), T>(rx[c], j, A);
+                if (EXACT) ry[EXACT ? (int)c : 0] = policy_cut<(LANES * CH > 16), T>(ry[EXACT ? (int)c : 0], j, A);
+            }
         });
         float m[2] = {PL_LOWEST, PL_LOWEST}, s[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
         pieces([&](auto c, int j) { P::max(rx[c], ry[EXACT ? (int)c : 0], r.a - j, m, s[4]); });
@@ -486,11 +514,10 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         }
         if (there && q.grad) {
             T *const d = (T *)q.grad + (int64_t)row * q.grad_ld;
-            const bool vec = policy_mis(d) == mis;
             pieces([&](auto i, int j) {
                 float o[V];
                 P::grad(rx[i], ry[EXACT ? (int)i : 0], z, zr, c, r.a - j, o);
-                if (j < A) policy_put(d, o, j, A, vec);
+                if (j < A) policy_put(d, o, j, A);
             });
         }
     }
@@ -523,7 +550,7 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     uint4 rx[CH], ry[EXACT ? CH : 1];
     const T *x = nullptr, *y = nullptr;                             // the row that is being loaded
     int mis = 0;
-    bool same = false, live = false;
+    bool live = false;
     double w = 0.0;
     auto start = [&](int64_t row) {
         w = row < rows ? uniform(policy_weight(q, (int)row, w_all, w_in, few)) : 0.0;
@@ -532,13 +559,11 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         x = (const T *)q.logits + row * q.ld;
         y = EXACT ? (const T *)q.ref_logits + row * q.ref_ld : nullptr;
         mis = policy_mis(x);
-        same = EXACT && policy_mis(y) == mis;
     };
     auto request = [&](auto i) {
         const int j = ((int)i * BLOCK + tid) * V - mis;
-        const bool whole = j >= 0 && j + V <= A;
-        rx[i] = !live || j >= A ? policy_none<T>() : whole ? *(const uint4 *)(x + j) : policy_edge(x, j, A);
-        if (EXACT) ry[EXACT ? (int)i : 0] = !live || j >= A ? policy_none<T>() : whole && same ? *(const uint4 *)(y + j) : policy_edge(y, j, A);
+        rx[i] = live && j < A ? policy_cut<true, T>(policy_load<true>(x, j, A), j, A) : policy_none<T>();
+        if (EXACT) ry[EXACT ? (int)i : 0] = live && j < A ? policy_cut<true, T>(policy_load<true>(y, j, A), j, A) : policy_none<T>();
     };
     start(blockIdx.x);
     static_for<CH>([&](auto i) { if (i < used) request(i); });
@@ -558,7 +583,8 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
                     float n[2] = {u.m[0], u.m[1]};
                     static_for<GROUP>([&](auto e) {
                         constexpr int i = decltype(g)::value * GROUP + decltype(e)::value;
-                        if (i < used) P::max(rx[i], ry[EXACT ? i : 0], centred ? -1 : r.a - ((i * BLOCK + tid) * V - mis_row), n, xa);
+                        const int j = (i * BLOCK + tid) * V - mis_row;
+                        if (i < used) P::max(rx[i], ry[EXACT ? i : 0], centred ? -1 : r.a - j, n, xa);
                     });
                     u.turn(n);
                     static_for<GROUP>([&](auto e) {
@@ -597,7 +623,6 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
             sum[3] += w_row * (double)c.clipped;
         }
         T *const d = q.grad ? (T *)q.grad + row * q.grad_ld : nullptr;
-        const bool vec = policy_mis(d) == mis_row;
         start(row + gridDim.x);
         static_for<CH>([&](auto i) {
             if (i < used) {
@@ -605,7 +630,7 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
                     const int j = ((int)i * BLOCK + tid) * V - mis_row;
                     float o[V];
                     P::grad(rx[i], ry[EXACT ? (int)i : 0], z, u.zr, c, r.a - j, o);
-                    if (j < A) policy_put(d, o, j, A, vec);
+                    if (j < A) policy_put(d, o, j, A);
                 }
                 request(i);
             }
@@ -619,7 +644,7 @@ k_policy_ring(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
 // A row that does not fit: one workgroup, two sweeps. The first keeps a running maximum per lane, its sums scaled anew where the
 // maximum of the next CH pieces is larger; the second reads the row again, from the caches where the rows in flight fit them.
 template <class T, bool EXACT, int BLOCK, int CH>
-__global__ void __launch_bounds__(BLOCK)
+__global__ void __launch_bounds__(BLOCK, BLOCK == 512 ? 5 : 1)
 k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
 {
     using P = PolicyPiece<T, EXACT, true>;
@@ -637,15 +662,16 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
         T *const d = q.grad ? (T *)q.grad + (int64_t)row * q.grad_ld : nullptr;
         const T *const x = (const T *)q.logits + (int64_t)row * q.ld, *const y = EXACT ? (const T *)q.ref_logits + (int64_t)row * q.ref_ld : nullptr;
         const int mis = policy_mis(x);
-        const bool same = EXACT && policy_mis(y) == mis, vec = d && policy_mis(d) == mis;
         if (w == 0.0) {
             if (tid == 0 && q.logp) q.logp[row] = 0.f;
             if (d) policy_clear(d, A, tid, BLOCK);
             continue;
         }
         const PolicyRow r = policy_inputs(q, row, w, tid == 0);
-        auto piece = [&](const T *v, bool aligned, int j) {
-            return aligned && j >= 0 && j + V <= A ? *(const uint4 *)(v + j) : j < A ? policy_edge(v, j, A) : policy_none<T>();
+        auto piece = [&](const T *v, int j) { return j < A ? policy_load<true>(v, j, A) : policy_none<T>(); };
+        auto cut = [&](uint4 (&r)[CH], int j0) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) if (const int j = j0 + c * BLOCK * V; j < A) r[c] = policy_cut<true, T>(r[c], j, A);
         };
         PolicyRunning<EXACT, true> u(k);
         float xa = 0.f;
@@ -654,9 +680,11 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int j = j0 + c * BLOCK * V;
-                rx[c] = piece(x, true, j);
-                if (EXACT) ry[c] = piece(y, same, j);
+                rx[c] = piece(x, j);
+                if (EXACT) ry[c] = piece(y, j);
             }
+            cut(rx, j0);
+            if (EXACT) cut(ry, j0);
             float n[2] = {u.m[0], u.m[1]};
 #pragma unroll
             for (int c = 0; c < CH; ++c) P::max(rx[c], ry[c], r.a - (j0 + c * BLOCK * V), n, xa);
@@ -686,15 +714,19 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     const int j = j0 + i * BLOCK * V;
-                    rx[i] = dead ? policy_none<T>() : piece(x, true, j);
-                    if (EXACT) ry[i] = dead ? policy_none<T>() : piece(y, same, j);
+                    rx[i] = dead ? policy_none<T>() : piece(x, j);
+                    if (EXACT) ry[i] = dead ? policy_none<T>() : piece(y, j);
+                }
+                if (!dead) {
+                    cut(rx, j0);
+                    if (EXACT) cut(ry, j0);
                 }
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     const int j = j0 + i * BLOCK * V;
                     float o[V];
                     P::grad(rx[i], ry[i], u.z, u.zr, c, r.a - j, o);
-                    if (j < A) policy_put(d, o, j, A, vec);
+                    if (j < A) policy_put(d, o, j, A);
                 }
             }
     }
@@ -740,9 +772,9 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
 //   4096 bf16 logits: 64 lanes x 8 pieces 4.8 TB/s, 256 x 4 (two pieces each, two barriers per row) 3.6
 //   32768 bf16: 512 x 8 4.7, two sweeps 3.7;  65536 bf16: ring of 512 4.7, one workgroup of 1024 without loading ahead 3.8, two sweeps 3.7
 //   128256 bf16: ring of 1024 4.0 (4.4 where rows fill the CUs evenly), not loading ahead 3.2, two sweeps 3.6
-//   65536 fp32: ring 4.5, two sweeps 4.1;  32768 fp32 with a reference: 4.7 from the ring, 3.3 by two sweeps
-// bf16 with a reference is bound by its arithmetic (two exponentials, 35 instructions per pair): from 32 KB on two sweeps by four
-// workgroups per CU reach 3.7-3.9 TB/s, the ring, which spills there, 2.9.
+//   32000 fp32: ring 5.1, two sweeps 4.2;  32000 fp32 with a reference: ring 4.8, two sweeps 3.3
+// bf16 with a reference is bound by its arithmetic (two exponentials, 35 instructions per pair): from 32 KB on two sweeps by three
+// workgroups per CU reach 3.4-3.8 TB/s, the ring, which spills there, 2.9.
 template <class T, bool EXACT>
 static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)
 {
@@ -774,7 +806,7 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
     else if (pieces <= 512) held(N(64), N(8));
     else if (pieces <= 1024) held(N(256), N(4));
     else if (pieces <= 2048) held(N(256), N(8));
-    else if constexpr (HEAVY) go(k_policy_stream<T, EXACT, 512, 4>, 512, 1);
+    else if constexpr (HEAVY) go(k_policy_stream<T, EXACT, 512, 2>, 512, 1);
     else if (pieces <= 4096) held(N(512), N(8));
     else if constexpr (EXACT) {
         if (pieces <= 8192) ring(N(1024), N(8));

@@ -521,8 +521,7 @@ class Sol:
         """Clipped policy loss with KL term and entropy bonus of logits [B][G][T][A] (float32 or bfloat16, rows evenly spaced),
         forward and gradient. action_ids int32, adv / old_logp / ref_logp float32 [B][G][T] or None, ref_logits like logits or
         None, eff int32 [B][T] or None. Returns dict of device tensors: loss [1], stats [4] (policy term, KL, entropy, clipped
-        share), logp [B][G][T], grad [B][G][T][A] (grad_out if given, which may be logits itself; None if want_grad is false; of padded
-        logits, rows with up to seven unused elements between them)."""
+        share), logp [B][G][T], grad [B][G][T][A] (grad_out if given, which may be logits itself; None if want_grad is false)."""
         here, dtype, shape = torch.cuda.current_device(), logits.dtype, logits.shape
         code = _CODE.get(dtype)
         if code is None or len(shape) != 4 or logits.get_device() != here:
@@ -543,11 +542,7 @@ class Sol:
                 _like(grad_out, logits, "grad_out")
                 grad_ld = _row_step(grad_out, "grad_out")
             else:
-                # rows of padded logits begin at other distances from 16 bytes than packed ones would: the gradient's as the logits' do
-                gap = (ld - A) % 8
-                grad_out, grad_ld = logits.new_empty((B, G, T, A + gap)), A + gap
-                if gap:
-                    grad_out = grad_out[..., :A]
+                grad_out, grad_ld = logits.new_empty(shape), A
             grad = grad_out.data_ptr()
         else:
             grad_out = None
