@@ -17,8 +17,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsol.so")
-LISTS_SRC = os.path.join(CSRC, "sol_lists.cpp")       # the binding's lists of torch tensors: compiled for the host against torch's headers
-LISTS_LIB = os.path.join(HERE, "libsol_lists.so")
+TORCH_SRC = os.path.join(CSRC, "sol_torch.cpp")       # the binding's part in C++: an extension module compiled against torch's headers
+TORCH_LIB = os.path.join(HERE, "sol_torch.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -52,26 +52,26 @@ def _compile(src, verbose):
     subprocess.run(cmd, check=True)
 
 
-def build_lists(force: bool = True, verbose: bool = False) -> str:
-    if not force and os.path.exists(LISTS_LIB) and os.path.getmtime(LISTS_LIB) >= os.path.getmtime(LISTS_SRC):
-        return LISTS_LIB
+def build_torch(force: bool = True, verbose: bool = False) -> str:
+    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= max(os.path.getmtime(p) for p in [TORCH_SRC] + headers()):
+        return TORCH_LIB
     import sysconfig
 
     import torch
     root = os.path.join(os.path.dirname(torch.__file__))
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], "-o", LISTS_LIB, LISTS_SRC, "-L" + os.path.join(root, "lib"), "-ltorch_python",
+           "-isystem", sysconfig.get_paths()["include"], "-o", TORCH_LIB, TORCH_SRC, "-L" + os.path.join(root, "lib"), "-ltorch_python",
            "-ltorch_cpu", "-ltorch", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    return LISTS_LIB
+    return TORCH_LIB
 
 
 def build(force: bool = True, verbose: bool = False) -> str:
     if not force and not is_stale():
-        build_lists(False, verbose)
+        build_torch(False, verbose)
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     newest_header = max(os.path.getmtime(p) for p in headers())
@@ -85,7 +85,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    build_lists(force, verbose)
+    build_torch(force, verbose)
     return LIB
 
 

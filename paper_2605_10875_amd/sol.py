@@ -224,66 +224,35 @@ def _i32(t):
     return t
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+_torch_part = None
 
 
-def _at(t, dtype, shape, here, what):
-    """Address of a contiguous tensor of device `here`, None if there is none."""
+def _native():
+    """The binding's part in C++ (csrc/sol_torch.cpp): built, as the library is, if it has never been."""
+    global _torch_part
+    if _torch_part is None:
+        import importlib.machinery
+        import importlib.util
+        if not os.path.exists(_build.TORCH_LIB):
+            _build.build_torch()
+        loader = importlib.machinery.ExtensionFileLoader("sol_torch", _build.TORCH_LIB)
+        spec = importlib.util.spec_from_file_location("sol_torch", _build.TORCH_LIB, loader=loader)
+        _torch_part = importlib.util.module_from_spec(spec)
+        loader.exec_module(_torch_part)
+    return _torch_part
+
+
+def _address(fn):
+    return C.cast(fn, C.c_void_p).value
+
+
+def _at(t, dtype, here, what):
+    """Address of a contiguous tensor of one element on device `here`, None if there is none."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or t.get_device() != here or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the current device is needed")
+    if t.dtype != dtype or t.numel() != 1 or t.get_device() != here:
+        raise ValueError(f"{what}: one {dtype} element on the current device is needed")
     return t.data_ptr()
-
-
-def _like(t, logits, what):
-    if t.shape != logits.shape or t.dtype != logits.dtype or t.get_device() != logits.get_device():
-        raise ValueError(f"{what}: not like logits")
-
-
-def _row_step(t, what):
-    """Elements from one row of t ([..][A], rows evenly spaced) to the next."""
-    A = t.shape[-1]
-    if t.is_contiguous():
-        return A
-    _need(A == 1 or t.stride(-1) == 1, f"{what}: the elements of a row have to be adjacent")
-    step, rows = 0, 1
-    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if size != 1:
-            step = step or stride
-            _need(rows == 1 or stride == step * rows, f"{what}: the rows have to be evenly spaced")
-            rows *= size
-    step = step or A
-    _need(step >= A, f"{what}: the rows overlap")
-    return step
-
-
-_lists = None
-
-
-def _tensor_lists(lists, names, types, typed):
-    """Host array of records for lists of as many tensors each (None: a list that is not there): addresses, elements, type of the
-    list `typed`. types: 1 float32, 2 bfloat16, 3 either."""
-    global _lists
-    if _lists is None:
-        if not os.path.exists(_build.LISTS_LIB):
-            _build.build_lists()
-        L = C.PyDLL(_build.LISTS_LIB)
-        L.sol_tensor_lists.restype = C.c_int64
-        L.sol_tensor_lists.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
-        _lists = L.sol_tensor_lists
-    n, k = len(lists[0]), len(lists)
-    words = (C.c_int64 * (n * (k + 2)))()
-    rc = _lists(lists, n, (C.c_int32 * k)(*types), typed, torch.cuda.current_device(), words)
-    if rc:
-        _need(rc > 0, "the lists have to be sequences of the same length")
-        rc -= 1
-        which, at, kind = rc // 8 % 16, rc // 128, {1: "float32", 2: "bfloat16", 3: "float32 or bfloat16"}
-        raise ValueError(f"{names[which]}[{at}]: " + ("a tensor is needed", f"{kind[types[which]]} is needed", "not on the current device",
-                                                      "a contiguous tensor is needed", f"not as many elements as {names[0]}[{at}]")[rc % 8])
-    return words, n
 
 
 def _used_on(stream, *ts):
@@ -294,7 +263,6 @@ def _used_on(stream, *ts):
                 t.record_stream(stream)
 
 
-_CODE = {torch.float32: F32, torch.bfloat16: BF16}
 MEANS = {"steps": 0, "schedules": 1}
 
 
@@ -312,6 +280,7 @@ class Sol:
         if rc:
             raise SolError(rc, (self.L.sol_last_error(None) or b"").decode())
         self._ws = None
+        self._policy = None
 
     def close(self):
         if self.handle:
@@ -522,48 +491,26 @@ class Sol:
         forward and gradient. action_ids int32, adv / old_logp / ref_logp float32 [B][G][T] or None, ref_logits like logits or
         None, eff int32 [B][T] or None. Returns dict of device tensors: loss [1], stats [4] (policy term, KL, entropy, clipped
         share), logp [B][G][T], grad [B][G][T][A] (grad_out if given, which may be logits itself; None if want_grad is false)."""
-        here, dtype, shape = torch.cuda.current_device(), logits.dtype, logits.shape
-        code = _CODE.get(dtype)
-        if code is None or len(shape) != 4 or logits.get_device() != here:
-            raise ValueError("logits: [B][G][T][A] of float32 or bfloat16 on the current device is needed")
-        if mean not in MEANS or action_ids is None:
-            raise ValueError("mean has to be 'steps' or 'schedules', and action_ids are needed")
-        B, G, T, A = shape
-        steps, n, f32, i32 = shape[:3], B * G * T, torch.float32, torch.int32
-        ids, eff = _at(action_ids, i32, steps, here, "action_ids"), _at(eff, i32, (B, T), here, "eff")
-        adv, old_logp = _at(adv, f32, steps, here, "adv"), _at(old_logp, f32, steps, here, "old_logp")
-        ref_logp, ref, ref_ld, grad, grad_ld = _at(ref_logp, f32, steps, here, "ref_logp"), None, 0, None, 0
-        ld = A if logits.is_contiguous() else _row_step(logits, "logits")
-        if ref_logits is not None:
-            _like(ref_logits, logits, "ref_logits")
-            ref, ref_ld = ref_logits.data_ptr(), _row_step(ref_logits, "ref_logits")
-        if want_grad:
-            if grad_out is not None:
-                _like(grad_out, logits, "grad_out")
-                grad_ld = _row_step(grad_out, "grad_out")
-            else:
-                grad_out, grad_ld = logits.new_empty(shape), A
-            grad = grad_out.data_ptr()
-        else:
-            grad_out = None
-        # one allocation: loss, stats, log-probabilities and the workspace behind them
-        need = self.L.sol_policy_workspace_bytes(B, G, T)
-        room = torch.empty if n else torch.zeros
-        out = room(5 + n + need // 4 + 1, dtype=f32, device="cuda")
-        loss, stats, logp, _ = out.split_with_sizes((1, 4, n, need // 4 + 1))
-        cfg, at = PolicyCfg(clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean]), out.data_ptr()
-        rc = self.L.sol_policy_loss(self.handle, logits.data_ptr(), code, ld, ids, adv, old_logp, ref_logp, ref, ref_ld, eff, C.byref(cfg), B, G,
-                                    T, A, at, at + 4, at + 20, grad, grad_ld, at + 20 + 4 * n, need, _stream(stream))
-        if rc:
-            self._check(rc)
+        if mean not in MEANS:
+            raise ValueError("mean: 'steps' or 'schedules'")
+        if self._policy is None:
+            self._policy = (_native().policy_loss, _address(self.L.sol_policy_loss), _address(self.L.sol_policy_workspace_bytes))
+        call, entry, sizes = self._policy
+        here = torch.cuda.current_device()
+        got = call(entry, sizes, self.handle.value or 0, here, _stream(stream).value or 0, logits, action_ids, adv, old_logp, ref_logp, ref_logits, eff,
+                   want_grad, grad_out, clip[0], clip[1], kl_coef, entropy_coef, temperature, scale, MEANS[mean])
+        if type(got) is int:
+            self._check(got)
+        loss, stats, logp, grad, out = got
         if stream is not None:
-            _used_on(stream, out, grad_out)
-        return {"loss": loss, "stats": stats, "logp": logp.view(steps), "grad": grad_out}
+            _used_on(stream, out, grad)
+        return {"loss": loss, "stats": stats, "logp": logp, "grad": grad}
 
     def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
         """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
         [1] on the device; scale: the gradients are multiplied by coef in place. Nothing is synchronised."""
-        words, n = _tensor_lists((grads,), ("grads",), (3,), 0)
+        words = _native().tensor_lists((grads,), ("grads",), (3,), 0, torch.cuda.current_device())
+        n = len(grads)
         out = torch.empty(2, dtype=torch.float32, device="cuda")
         need = self.L.sol_grad_clip_workspace_bytes(n)
         ws = torch.empty(need, dtype=torch.uint8, device="cuda")
@@ -578,11 +525,11 @@ class Sol:
         """AdamW on lists of contiguous tensors: params, exp_avg, exp_avg_sq float32, grads float32 or bfloat16, copies bfloat16
         (rounded parameters for the forward pass) or None. step: int32 [1] on the device, the number of this update from 1; lr: a
         number, or float32 [1] on the device; coef: grad_clip's coefficient, by which the gradients are multiplied on the way, or None."""
-        words, n = _tensor_lists((params, exp_avg, exp_avg_sq, grads, copies), ("params", "exp_avg", "exp_avg_sq", "grads", "copies"),
-                                 (1, 1, 1, 3, 2), 3)
-        here, by_tensor = torch.cuda.current_device(), isinstance(lr, torch.Tensor)
-        step, coef, rate = (_at(t, dtype, (1,), here, what) for t, dtype, what in
-                            ((step, torch.int32, "step"), (coef, torch.float32, "coef"), (lr if by_tensor else None, torch.float32, "lr")))
+        here, by_tensor, n = torch.cuda.current_device(), isinstance(lr, torch.Tensor), len(params)
+        words = _native().tensor_lists((params, exp_avg, exp_avg_sq, grads, copies), ("params", "exp_avg", "exp_avg_sq", "grads", "copies"),
+                                       (1, 1, 1, 3, 2), 3, here)
+        step, coef = _at(step, torch.int32, here, "step"), _at(coef, torch.float32, here, "coef")
+        rate = _at(lr, torch.float32, here, "lr") if by_tensor else None
         cfg = AdamwCfg(0.0 if by_tensor else lr, betas[0], betas[1], eps, weight_decay)
         self._check(self.L.sol_adamw_step(self.handle, words, n, C.byref(cfg), step, rate, coef, _stream(stream)))
 
