@@ -100,7 +100,8 @@ template <int BLOCK> __device__ __forceinline__ double up_block_sum(double v, do
     return t;
 }
 
-// Squares are summed in 64 bits: neither do they overflow, nor does the number of elements show. Bound by reading the gradients once.
+// Squares are summed in 64 bits: neither do they overflow, nor does the number of elements show. Bound by reading the gradients once: 1.24 G
+// bf16 elements 415 us, 5.9 TB/s (one 8-byte load in flight per thread: 1096).
 template <class T>
 __global__ void __launch_bounds__(UP_BLOCK) k_grad_squares(ClipList l, double *__restrict__ partial)
 {
@@ -141,6 +142,8 @@ k_grad_norm(const double *__restrict__ partial, int64_t n, double max_norm, doub
     }
 }
 
+// Every gradient read and written once more: 1.24 G bf16 elements 880 us, 5.6 TB/s with what the norm has left in the memory-side cache (2048
+// looping workgroups 1110).
 template <class T>
 __global__ void __launch_bounds__(UP_BLOCK) k_grad_scale(ClipList l, const float *__restrict__ coef)
 {
@@ -175,6 +178,8 @@ __device__ __forceinline__ double pow_int(double b, int t)
     return r;
 }
 
+// All streams once, 28 bytes per element: 243 M elements with bf16 gradients and copies 1200 us, 5.7 TB/s (16384 looping workgroups 1455).
+// Roundings: the moments and the parameter to 32 bits, the copy to bf16 from the rounded parameter.
 template <class T>
 __global__ void __launch_bounds__(UP_BLOCK)
 k_adamw(AdamList l, AdamCfg a, const int32_t *__restrict__ step, const float *__restrict__ lr_dev, const float *__restrict__ coef, int *flags)
