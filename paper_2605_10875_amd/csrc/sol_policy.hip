@@ -96,7 +96,7 @@ k_policy_weights(const int32_t *__restrict__ n, int B, int G, int by_schedule, d
 }
 
 // exp(u) - u - 1: by its series near 0, where the difference would keep a few bits only (|u| < 0.5: the first term left out
-// is below 2^-33 of the sum)
+// is below 2^-33 of the sum), without the difference where u is infinite
 __device__ __forceinline__ float policy_kl(float u)
 {
     float s = 1.f / 3628800.f;
@@ -108,7 +108,7 @@ __device__ __forceinline__ float policy_kl(float u)
     s = s * u + 1.f / 24.f;
     s = s * u + 1.f / 6.f;
     s = s * u + 0.5f;
-    return fabsf(u) < 0.5f ? s * u * u : expf(u) - u - 1.f;
+    return fabsf(u) < 0.5f ? s * u * u : u > 60.f ? expf(u) : expf(u) - u - 1.f;
 }
 
 // log x for 2^-1000 < x < 2^1000: mantissa in [sqrt 1/2, sqrt 2), log f = 2 artanh((f - 1) / (f + 1)), whose argument is at most
@@ -174,12 +174,12 @@ __device__ __forceinline__ PolicyCoef policy_row(const PolicyScalars &pc, const 
     } else if (has_ref) {
         const float u = (float)((double)r.ref - logp);
         c.kl = policy_kl(u);
-        G -= beta * (u + c.kl);                                     // 1 - exp(u)
+        G -= times(beta, u + c.kl);                                 // 1 - exp(u); an infinite KL without a coefficient is no one's
     }
     c.clipped = clipped ? 1.f : 0.f;
     const float w = (float)(r.w * pc.factor), ent = (float)pc.ent;
     c.hot = w * G;
-    c.alpha = -w * (G + ent * u_mean + (exact_kl ? beta * k_mean : 0.f)) * inv;
+    c.alpha = -w * (G + ent * u_mean + (exact_kl ? times(beta, k_mean) : 0.f)) * inv;
     c.gamma = w * ent * ln2 * inv;
     c.kappa = exact_kl ? w * beta * ln2 * inv : 0.f;
     return c;
@@ -385,7 +385,7 @@ template <class T, bool EXACT, bool SUB> struct PolicyPiece {
         for (int i = 0; i < V; ++i) {
             const float t = policy_t<SUB>(f[i], z), e = __builtin_amdgcn_exp2f(t);
             float h = __builtin_fmaf(c.gamma, t, c.alpha);
-            if (EXACT) h = __builtin_fmaf(c.kappa, t - policy_t<SUB>(g[i], zr), h);
+            if (EXACT) h += times(c.kappa, t - policy_t<SUB>(g[i], zr));
             o[i] = times(e, h);
         }
         if ((unsigned)at < (unsigned)V)
@@ -417,7 +417,9 @@ template <bool EXACT, bool SUB> struct PolicyRunning {
         const PolicyScale y = policy_scale<SUB>(n[0], k), yr = EXACT ? policy_scale<SUB>(n[1], k) : y;
         if (s[0] > 0.f) {                                           // t' = t + up
             const float up = policy_t<SUB>(m[0], y) - policy_t<SUB>(m[0], z), f = __builtin_amdgcn_exp2f(up);
-            if (EXACT) s[3] = times(f, __builtin_fmaf(s[0], up - (policy_t<SUB>(m[1], yr) - policy_t<SUB>(m[1], zr)), s[3]));
+            // (no finite reference logit yet: s[3] is infinite and stays it)
+            const float upr = EXACT && m[1] > PL_LOWEST ? policy_t<SUB>(m[1], yr) - policy_t<SUB>(m[1], zr) : 0.f;
+            if (EXACT) s[3] = times(f, __builtin_fmaf(s[0], up - upr, s[3]));
             s[1] = times(f, __builtin_fmaf(s[0], up, s[1]));
             s[0] = times(f, s[0]);
         }
@@ -762,7 +764,7 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
 #pragma unroll
             for (int i = 0; i < PL_FINISH / 64; ++i) v[e] += red[i][e];
         }
-        *loss = (float)(pc.scale * (v[0] + pc.kl * v[1] - pc.ent * v[2]));
+        *loss = (float)(pc.scale * (v[0] + (pc.kl > 0.0 ? pc.kl * v[1] : 0.0) - pc.ent * v[2]));
         if (stats)
 #pragma unroll
             for (int e = 0; e < 4; ++e) stats[e] = (float)v[e];

@@ -345,6 +345,32 @@ def test_two_streams_at_once(ctx):
             assert torch.equal(nc[0], norms[k][0]) and torch.equal(nc[1], norms[k][1])
 
 
+@pytest.mark.parametrize("A", [5, 64, 700, 5000, 20001, 40001, 140001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_a_reference_that_forbids_more_than_the_policy(ctx, A, dtype):
+    """KL is infinite; without a coefficient it shows in the statistics alone."""
+    x, ids, kw = _case(1, 2, 3, A, dtype, kl="logits", seed=22)
+    kw["ref_logits"][0, 1, 1, A // 2] = -np.inf
+    kw["ref_logits"][0, 0, 2, : A // 2 + 1] = -np.inf
+    got = _run(ctx, x, ids, {**kw, "kl_coef": 0.0})
+    bare = _run(ctx, x, ids, {k: v for k, v in {**kw, "kl_coef": 0.0}.items() if k != "ref_logits"})
+    assert host(got["stats"])[1] == np.inf and np.isfinite(host(got["loss"])).all() and np.isfinite(host(got["grad"])).all()
+    np.testing.assert_allclose(host(got["grad"]), host(bare["grad"]), rtol=2 * HALF[dtype] + 1e-5, atol=1e-9)      # (sums in another order)
+    np.testing.assert_allclose(float(got["loss"]), float(bare["loss"]), rtol=1e-5, atol=1e-6)
+    got = _run(ctx, x, ids, kw)
+    assert host(got["stats"])[1] == np.inf and float(got["loss"]) == np.inf
+    rows = torch.isfinite(got["grad"].float()).all(-1)[0].cpu().numpy()
+    assert rows.tolist() == [[True, True, False], [True, False, True]]
+    # the estimate, of an action that the policy forbids
+    x[0, 0, 0, A - 1] = -np.inf
+    ids[0, 0, 0] = A - 1
+    kw = {k: v for k, v in kw.items() if k != "ref_logits"}
+    got = _run(ctx, x, ids, {**kw, "ref_logp": np.full((1, 2, 3), -2.0, np.float32)})
+    assert host(got["stats"])[1] == np.inf and float(got["loss"]) == np.inf and np.isfinite(host(got["grad"])[0, 1]).all()
+    got = _run(ctx, x, ids, {**kw, "kl_coef": 0.0, "ref_logp": np.full((1, 2, 3), -2.0, np.float32)})
+    assert np.isfinite(host(got["loss"])).all() and np.isfinite(host(got["grad"])).all()
+
+
 @pytest.mark.parametrize("temperature", [2.0 ** -20, 1e-3, 50.0, 2.0 ** 20])
 @pytest.mark.parametrize("A", [9, 5000])
 def test_temperatures_at_the_ends(ctx, temperature, A):
