@@ -290,15 +290,16 @@ int sol_reward_advantages(sol_ctx *ctx, const float *nll, const int32_t *action_
  * any effective row the loss is 0. A logit of -inf forbids its action (p = 0, gradient 0); a row without an allowed action gives 0
  * everywhere and logp -inf, and counts in the mean. NaN and +inf make the row, and the loss, NaN. An action id outside [0, A) counts
  * as action 0 and sets the bad-action flag.
- * logits: device [B][G][T] rows of A elements of dtype (sol_dtype), ld >= A elements apart; ref_logits likewise, ref_ld apart. adv (NULL:
- * 0), old_logp, ref_logp: device float [B][G][T]; action_ids: device int32 [B][G][T]; eff: device int32 [B][T] or NULL (all). Outputs,
- * device: loss_out float [1]; stats_out float [4], the means of pg, KL, H and of the share of clipped rows, or NULL; logp_out float
- * [B][G][T], the actions' log-probabilities (the next update's old_logp), or NULL; grad_out rows of A elements of dtype, grad_ld
- * apart, or NULL (loss alone). grad_out may be logits itself with grad_ld == ld; any other overlap with the logits is refused, and
- * elements between the rows are left as they are. Where the reference forbids an action that the policy allows, KL is infinite, and with
- * kl_coef > 0 the row's gradient is not finite. A row's elements are summed in 32 bits, its log-probability, the test of the ratio's bounds and the sums
- * over the rows are in 64; a gradient is rounded once. The order of a row's sums depends on A, on the number of elements that the row
- * begins behind a 16-byte boundary and on nothing else. Workspace: sol_policy_workspace_bytes(B, G, T), device memory of any alignment.
+ * logits: device [B][G][T] rows of A elements of dtype (sol_dtype), ld >= A elements apart; ref_logits likewise, ref_ld apart. adv
+ * (NULL: 0), old_logp, ref_logp: device float [B][G][T]; action_ids: device int32 [B][G][T]; eff: device int32 [B][T] or NULL (all).
+ * Outputs, device: loss_out float [1]; stats_out float [4], the means of pg, KL, H and of the share of clipped rows, or NULL; logp_out
+ * float [B][G][T], the actions' log-probabilities (the next update's old_logp), none of the inputs, or NULL; grad_out rows of A
+ * elements of dtype, grad_ld apart, or NULL (loss alone). grad_out may be logits itself with grad_ld == ld; any other overlap with the
+ * logits is refused, and elements between the rows are left as they are. Where the reference forbids an action that the policy allows,
+ * KL is infinite, and with kl_coef > 0 the row's gradient is not finite. A row's elements are summed in 32 bits, its log-probability,
+ * the test of the ratio's bounds and the sums over the rows are in 64; a gradient is rounded once. The order of a row's sums depends
+ * on A, on the number of elements that the row begins behind a 16-byte boundary and on nothing else. Workspace:
+ * sol_policy_workspace_bytes(B, G, T), device memory of any alignment.
  * B * G * T == 0 is a no-op (loss_out is left as it is); at most 2^31 - 1 rows of 2^30 actions. */
 #define SOL_MEAN_STEPS 0
 #define SOL_MEAN_SCHEDULES 1
@@ -336,7 +337,7 @@ int sol_grad_clip(sol_ctx *ctx, const sol_grad *grads, int n_tensors, double max
  * sol_device_status reports SOL_ERR_INVALID_ARG. lr: device float [1] in place of cfg.lr, or NULL. tensors: HOST array as in
  * sol_grad_clip; param, m, v: device float [n]; grad: device [n] of grad_dtype, read only; copy: device bf16 [n] or NULL, what a bf16
  * forward pass reads (parameters and moments stay in 32 bits: a bf16 parameter would lose updates below 2^-9 of its value). Tensors that
- * are written must not overlap each other or a gradient (refused). No workspace. */
+ * are written must not overlap each other or a gradient (refused); 2^37 elements each at most. No workspace. */
 typedef struct { float *param, *m, *v; const void *grad; void *copy; int64_t n; int32_t grad_dtype; int32_t reserved; } sol_adamw_tensor;
 typedef struct { double lr, beta1, beta2, eps, weight_decay; } sol_adamw_cfg;   /* betas in [0, 1), the others >= 0 */
 int sol_adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tensors, const sol_adamw_cfg *ac, const int32_t *step,

@@ -1006,7 +1006,9 @@ static int policy_loss(sol_ctx *ctx, const void *logits, int dtype, int64_t ld, 
         if (!(grad_out == logits && grad_ld == ld) && meet(g, span(logits, ld))) return fail(ctx, SOL_ERR_INVALID_ARG, "grad_out overlaps logits");
         if (ref_logits && meet(g, span(ref_logits, ref_ld))) return fail(ctx, SOL_ERR_INVALID_ARG, "grad_out overlaps ref_logits");
     }
-    if (logp_out && (logp_out == adv || logp_out == old_logp || logp_out == ref_logp)) return fail(ctx, SOL_ERR_INVALID_ARG, "logp_out must not alias an input");
+    auto of_steps = [&](const void *p) { return range_of(p, (uint64_t)rows * 4); };
+    for (const void *in : {(const void *)action_ids, (const void *)adv, (const void *)old_logp, (const void *)ref_logp})
+        if (logp_out && in && meet(of_steps(logp_out), of_steps(in))) return fail(ctx, SOL_ERR_INVALID_ARG, "logp_out overlaps an input");
     const size_t need = sol_policy_workspace_bytes(B, G, T);
     if (!workspace || ws_bytes < need) return fail(ctx, SOL_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
     if (const int rc = on_device(ctx)) return rc;
@@ -1091,6 +1093,7 @@ static int adamw_step(sol_ctx *ctx, const sol_adamw_tensor *tensors, int n_tenso
         const sol_adamw_tensor &t = tensors[i];
         auto which = [i] { return "tensor " + std::to_string(i); };
         if (t.n < 0 || (t.n > 0 && (!t.param || !t.m || !t.v || !t.grad))) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": no data");
+        if (t.n > (int64_t)CLIP_MOST) return fail(ctx, SOL_ERR_UNSUPPORTED, which() + ": more than 2^37 elements");
         if (t.grad_dtype != SOL_F32 && t.grad_dtype != SOL_BF16) return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": grad_dtype must be SOL_F32 or SOL_BF16");
         if (((uintptr_t)t.param | (uintptr_t)t.m | (uintptr_t)t.v) % 4 || (uintptr_t)t.grad % esize(t.grad_dtype) || (uintptr_t)t.copy % 2)
             return fail(ctx, SOL_ERR_INVALID_ARG, which() + ": not aligned to its elements");

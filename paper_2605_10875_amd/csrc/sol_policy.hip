@@ -65,9 +65,9 @@ __global__ void __launch_bounds__(PL_BLOCK)
 k_policy_count(const int32_t *__restrict__ eff, int B, int T, int32_t *__restrict__ n)
 {
     __shared__ int red[PL_BLOCK / 64];
-    for (int b = blockIdx.x; b < B; b += gridDim.x) {
+    for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {                // (B and T may be close to 2^31)
         int c = 0;
-        for (int t = threadIdx.x; t < T; t += PL_BLOCK) c += eff[(int64_t)b * T + t] != 0;
+        for (int64_t t = threadIdx.x; t < T; t += PL_BLOCK) c += eff[b * T + t] != 0;
         c = wave_sum_i(c);
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
         __syncthreads();
@@ -83,7 +83,7 @@ k_policy_weights(const int32_t *__restrict__ n, int B, int G, int by_schedule, d
 {
     __shared__ int64_t red[PL_BLOCK];
     int64_t c = 0;
-    for (int b = threadIdx.x; b < B; b += PL_BLOCK) c += by_schedule ? n[b] > 0 : n[b];
+    for (int64_t b = threadIdx.x; b < B; b += PL_BLOCK) c += by_schedule ? n[b] > 0 : n[b];
     red[threadIdx.x] = c;
     __syncthreads();
     for (int o = PL_BLOCK / 2; o > 0; o >>= 1) {
@@ -91,7 +91,7 @@ k_policy_weights(const int32_t *__restrict__ n, int B, int G, int by_schedule, d
         __syncthreads();
     }
     const double all = (double)red[0] * (double)G;
-    for (int b = threadIdx.x; b < B; b += PL_BLOCK)
+    for (int64_t b = threadIdx.x; b < B; b += PL_BLOCK)
         w[b] = policy_share(n[b], all, by_schedule);
 }
 
@@ -534,7 +534,7 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
     }
 }
 
-// A row in the registers of one workgroup per CU, CH pieces per lane of each of its 1024: too large for a second workgroup that would
+// A row in the registers of half a CU or a whole one, CH pieces per lane of 512 or 1024: too large for the other workgroups that would
 // work while this one waits for memory, so each piece of the next row is requested as soon as this row's gradient has left its
 // registers, and the sums start with the pieces that are there. Workgroups take rows in turn. 2664 rows of 128256 bf16 logits: 300 us, 4.6
 // TB/s; vector instructions fill 166 of them, and nothing is under way while the last pieces arrive and the row's sums are folded.
@@ -771,7 +771,7 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
     }
 }
 
-// The row's kernel by its number of 16-byte pieces. Rows of up to 32 KB (16 with a reference) stay in the registers of as few lanes as
+// The row's kernel by its number of 16-byte pieces. Rows of up to 64 KB (32 of bf16 with a reference) stay in the registers of as few lanes as
 // hold them, so that many rows are under way per CU and few lanes repeat a row's scalars; longer ones fill the registers of a CU by
 // one or two, and load ahead (k_policy_ring); what does not fit is read twice. Measured, 200 M logits (bytes read and written / time, of
 // 5.06 TB/s that a copy of 1 GiB reaches):
@@ -779,7 +779,7 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
 //   32768 bf16: 512 x 8 4.7, two sweeps 3.7;  65536 bf16: ring of 512 4.7, one workgroup of 1024 without loading ahead 3.8, two sweeps 3.7
 //   128256 bf16: ring of 1024 4.0 (4.4 where rows fill the CUs evenly), not loading ahead 3.2, two sweeps 3.6
 //   32000 fp32: ring 5.1, two sweeps 4.2;  32000 fp32 with a reference: ring 4.8, two sweeps 3.3
-// bf16 with a reference is bound by its arithmetic (two exponentials, 35 instructions per pair): from 32 KB on two sweeps by three
+// bf16 with a reference is bound by its arithmetic (two exponentials, 35 instructions per pair): from 32 KB on two sweeps by two
 // workgroups per CU reach 3.4-3.8 TB/s, the ring, which spills there, 2.9.
 template <class T, bool EXACT>
 static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_all, const double *w, double *partial, int rows, hipStream_t st)

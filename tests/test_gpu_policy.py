@@ -378,6 +378,59 @@ def test_temperatures_at_the_ends(ctx, temperature, A):
     _check(_run(ctx, x, ids, kw), _oracle(x, ids, kw), x, kw, _rel(x, kw))
 
 
+@pytest.mark.parametrize("A,rows,some,dtype,exact", [(64, 3 << 24, 96, torch.bfloat16, False), (65536, 3 << 14, 48, torch.bfloat16, False),
+                                                      (20000, 15 << 13, 60, torch.float32, True), (140000, 15 << 10, 60, torch.bfloat16, False),
+                                                      (20000, 15 << 13, 60, torch.bfloat16, True)])
+def test_offsets_past_32_bits(ctx, A, rows, some, dtype, exact):
+    """The last rows of over 2^31 logits, against a call of these rows alone: rows / some is a power of two, so that the weights are the same."""
+    torch.manual_seed(A)
+    assert rows * A > 2 ** 31 and rows % some == 0 and (rows // some) & (rows // some - 1) == 0
+    x = torch.empty(1, 1, rows, A, dtype=dtype, device="cuda").normal_()
+    ref = torch.empty_like(x).normal_() if exact else None
+    ids = torch.randint(0, A, (1, 1, rows), dtype=torch.int32, device="cuda")
+    adv = torch.randn(1, 1, rows, device="cuda")
+    kw = dict(clip=CLIP, entropy_coef=0.05, kl_coef=0.1 if exact else 0.0)
+    alone = ctx.policy_loss(x[:, :, -some:].clone(), ids[:, :, -some:].clone(), adv[:, :, -some:].clone(), ref_logits=ref[:, :, -some:].clone() if exact else None,
+                            scale=some / rows, **kw)
+    got = ctx.policy_loss(x, ids, adv, ref_logits=ref, grad_out=x, **kw)
+    assert torch.equal(got["logp"][:, :, -some:], alone["logp"]) and torch.equal(x[:, :, -some:], alone["grad"])
+    assert abs(float(got["loss"])) < np.inf and float(alone["grad"].float().abs().max()) > 0.0
+    assert ctx.device_status() == sol.OK
+
+
+def test_the_largest_number_of_rows(ctx):
+    """2^31 - 1 rows of two equal logits, the last one and some others not effective."""
+    B = 2 ** 31 - 1
+    x = torch.zeros(B, 1, 1, 2, dtype=torch.bfloat16, device="cuda")
+    eff = torch.ones(B, 1, dtype=torch.int32, device="cuda")
+    eff[-1] = 0
+    eff[5:1000] = 0
+    out = ctx.policy_loss(x, torch.zeros(B, 1, 1, dtype=torch.int32, device="cuda"), eff=eff, entropy_coef=1.0, grad_out=x)
+    logp, half = out["logp"].view(-1), float(np.float32(-np.log(2.0)))
+    assert float(logp[-1]) == 0.0 and int((logp == 0.0).sum()) == 996
+    assert float((logp[-3000:-1] - half).abs().max()) <= 2.0 ** -24 and float((logp[:5] - half).abs().max()) <= 2.0 ** -24
+    # 2^31 equal terms of 64 bits, 2^31 / 2048 of them in a row: 2^20 roundings of 2^-53, and each entropy's own few of 2^-24
+    assert abs(float(out["loss"]) + np.log(2.0)) < 2.0 ** -21
+    assert ctx.device_status() == sol.OK
+
+
+def test_log_probabilities_do_not_go_into_an_input(ctx):
+    x, ids, kw = _case(1, 2, 3, 8, seed=23)
+    buf, cfg = torch.zeros(32, device="cuda"), sol.PolicyCfg(0.2, 0.2, 0.0, 0.0, 1.0, 1.0, 0)
+    ws = torch.zeros(ctx.L.sol_policy_workspace_bytes(1, 2, 3), dtype=torch.uint8, device="cuda")
+    a = dev(ids)
+
+    def call(adv, logp, ids=a.data_ptr()):
+        return ctx.L.sol_policy_loss(ctx.handle, x.data_ptr(), sol.F32, x.stride(2), ids, adv, None, None, None, 0, None, sol.C.byref(cfg), 1, 2, 3, 8,
+                                     buf[31:].data_ptr(), None, logp, None, 0, ws.data_ptr(), ws.numel(), None)
+
+    for at in (8, 10, 13, 3):
+        assert call(buf[8:].data_ptr(), buf[at:].data_ptr()) == sol.ERR_INVALID_ARG, at
+    assert call(buf[8:].data_ptr(), a.data_ptr()) == sol.ERR_INVALID_ARG
+    assert call(buf[8:].data_ptr(), buf[14:].data_ptr()) == sol.OK and call(buf[8:].data_ptr(), buf[2:].data_ptr()) == sol.OK
+    assert ctx.device_status() == sol.OK
+
+
 def test_refusals(ctx):
     x, ids, kw = _case(1, 2, 3, 8, kl="logp", seed=12)
 

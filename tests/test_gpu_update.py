@@ -167,6 +167,50 @@ def test_a_gradient_may_serve_two_parameters(ctx):
     assert torch.equal(b[0], alone[0]) and torch.equal(b[3], alone[3])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_offsets_past_32_bits(ctx, dtype):
+    """One tensor of over 2^31 elements, that takes two places of a list: values that differ on both sides of its middle and at its end."""
+    n, mid = 2 ** 31 + 12345, 2 ** 31 - 7
+    g = torch.full((n,), 0.5, dtype=dtype, device="cuda")
+    g[mid:] = -0.25
+    g[-1] = 1024.0
+    want = (0.25 * mid + 0.0625 * (n - mid - 1) + 2.0 ** 20) ** 0.5
+    norm, coef = ctx.grad_clip([g[:100].clone(), g], 100.0, scale=False)
+    want = (want * want + 25.0) ** 0.5
+    assert abs(float(norm) - want) < 2.0 ** -23 * want                                # a rounding to 32 bits, and 2^31 / 2^19 of 64 bits
+    parts = ((0, mid, 0.5), (mid, n - 1, -0.25), (n - 1, n, 1024.0))
+    p, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    copy = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    step = torch.ones(1, dtype=torch.int32, device="cuda")
+    ctx.adamw_step([p], [g], [m], [v], step, 1e-2, coef=coef, copies=[copy])
+    for lo, hi, x in parts:                                                           # as a tensor of one element does
+        one = [torch.zeros(1, device="cuda") for _ in range(3)]
+        c = torch.zeros(1, dtype=torch.bfloat16, device="cuda")
+        ctx.adamw_step([one[0]], [torch.full((1,), x, dtype=dtype, device="cuda")], [one[1]], [one[2]], step, 1e-2, coef=coef, copies=[c])
+        assert float(one[0]) != 0.0
+        for big, small in ((p, one[0]), (m, one[1]), (v, one[2]), (copy, c)):
+            assert bool((big[lo:hi] == small).all()), (lo, hi)
+    del p, m, v, copy
+    _, coef = ctx.grad_clip([g], 100.0)
+    for lo, hi, x in parts:
+        assert bool((g[lo:hi] == (torch.tensor(x, device="cuda") * coef).to(dtype)).all()), (lo, hi)
+    assert ctx.device_status() == sol.OK
+
+
+def test_sizes_that_no_memory_holds(ctx):
+    """(from C: a record whose number of elements is garbage)"""
+    p, g, m, v = _states(64)
+    step = torch.ones(1, dtype=torch.int32, device="cuda")
+    out = torch.zeros(2 + 4096, device="cuda")
+    cfg = sol.AdamwCfg(1e-3, 0.9, 0.999, 1e-8, 0.0)
+    for n in (2 ** 37 + 1, 2 ** 61, 2 ** 62, 2 ** 63 - 1):
+        record = (sol.C.c_int64 * 7)(p.data_ptr(), m.data_ptr(), v.data_ptr(), g.data_ptr(), 0, n, 0)
+        assert ctx.L.sol_adamw_step(ctx.handle, record, 1, sol.C.byref(cfg), step.data_ptr(), None, None, None) == sol.ERR_UNSUPPORTED
+        record = (sol.C.c_int64 * 3)(g.data_ptr(), n, 0)
+        assert ctx.L.sol_grad_clip(ctx.handle, record, 1, 1.0, 0.0, 1, out.data_ptr(), out[1:].data_ptr(), out[2:].data_ptr(), 16384, None) == sol.ERR_UNSUPPORTED
+    assert ctx.device_status() == sol.OK
+
+
 def test_refusals(ctx):
     step = torch.ones(1, dtype=torch.int32, device="cuda")
     p, g, m, v = _states(64)
