@@ -61,37 +61,54 @@ template <int BLOCK> __device__ __forceinline__ void policy_count(const PolicyAr
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(PL_BLOCK)
-k_policy_count(const int32_t *__restrict__ eff, int B, int T, int32_t *__restrict__ n)
+// Many flags: LANES lanes count an input's, and each workgroup adds up its inputs'; then the shares. B and T may be close to 2^31. Bound by
+// latency at few inputs (8 of 2048 flags: 3 us each), by reading the flags at many.
+__device__ __forceinline__ int64_t policy_block_sum(int64_t v, int64_t *red)
 {
-    __shared__ int red[PL_BLOCK / 64];
-    for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {                // (B and T may be close to 2^31)
-        int c = 0;
-        for (int64_t t = threadIdx.x; t < T; t += PL_BLOCK) c += eff[b * T + t] != 0;
-        c = wave_sum_i(c);
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int i = 1; i < PL_BLOCK / 64; ++i) c += red[i];
-            n[b] = c;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int i = 0; i < PL_BLOCK / 64; ++i) v += red[i];
+    __syncthreads();
+    return v;
+}
+template <int LANES>
+__global__ void __launch_bounds__(PL_BLOCK)
+k_policy_count(const int32_t *__restrict__ eff, int B, int T, int by_schedule, int32_t *__restrict__ n, int64_t *__restrict__ part)
+{
+    constexpr int INPUTS = PL_BLOCK / LANES;
+    __shared__ int64_t red[PL_BLOCK / 64];
+    const int lane = threadIdx.x % LANES;
+    int64_t sum = 0;
+    for (int64_t first = (int64_t)blockIdx.x * INPUTS; first < B; first += (int64_t)gridDim.x * INPUTS) {
+        const int64_t b = first + threadIdx.x / LANES;
+        int64_t c = 0;
+        if (b < B)
+#pragma unroll 4
+            for (int64_t t = lane; t < T; t += LANES) c += eff[b * T + t] != 0;
+        if (LANES > 64) c = policy_block_sum(c, red);
+        else
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+        if (b < B && lane == 0) {
+            n[b] = (int32_t)c;
+            sum += by_schedule ? c > 0 : c;
         }
-        __syncthreads();
     }
+    sum = policy_block_sum(sum, red);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 __global__ void __launch_bounds__(PL_BLOCK)
-k_policy_weights(const int32_t *__restrict__ n, int B, int G, int by_schedule, double *__restrict__ w)
+k_policy_weights(const int32_t *__restrict__ n, const int64_t *__restrict__ part, int parts, int B, int G, int by_schedule, double *__restrict__ w)
 {
-    __shared__ int64_t red[PL_BLOCK];
+    __shared__ int64_t red[PL_BLOCK / 64];
     int64_t c = 0;
-    for (int64_t b = threadIdx.x; b < B; b += PL_BLOCK) c += by_schedule ? n[b] > 0 : n[b];
-    red[threadIdx.x] = c;
-    __syncthreads();
-    for (int o = PL_BLOCK / 2; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
-    }
-    const double all = (double)red[0] * (double)G;
-    for (int64_t b = threadIdx.x; b < B; b += PL_BLOCK)
+    for (int i = threadIdx.x; i < parts; i += PL_BLOCK) c += part[i];
+    const double all = (double)policy_block_sum(c, red) * (double)G;
+    for (int64_t b = (int64_t)blockIdx.x * PL_BLOCK + threadIdx.x; b < B; b += (int64_t)gridDim.x * PL_BLOCK)
         w[b] = policy_share(n[b], all, by_schedule);
 }
 
@@ -824,8 +841,8 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
     return grid;
 }
 
-// [partial sums][counts int32 B][weights double B]
-size_t policy_scratch_bytes(int B) { return (size_t)PL_GRID * 4 * sizeof(double) + (size_t)B * 16 + 64; }
+// [partial sums][partial counts int64][weights double B][counts int32 B]
+size_t policy_scratch_bytes(int B) { return (size_t)PL_GRID * (4 * sizeof(double) + sizeof(int64_t)) + (size_t)B * 12 + 64; }
 
 void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStream_t st)
 {
@@ -835,15 +852,27 @@ void launch_policy_loss(PolicyArgs q, const PolicyCfg &g, void *scratch, hipStre
     const bool aligned = (uintptr_t)q.logits % 16 == 0 && (q.ld % V == 0 || (int64_t)q.B * q.G * q.T == 1);
     q.pieces = (int)(((int64_t)q.A + (aligned ? 0 : V - 1) + V - 1) / V);
     q.by_schedule = g.by_schedule;
-    double *partial = (double *)scratch, *w = partial + 4 * PL_GRID;
+    double *partial = (double *)scratch;
+    int64_t *part = (int64_t *)(partial + 4 * PL_GRID);
+    double *w = (double *)(part + PL_GRID);
     int32_t *n = (int32_t *)(w + q.B);
     const PolicyScalars pc{1.0 / g.temperature, log(1.0 - g.clip_low), log(1.0 + g.clip_high), g.scale / g.temperature, g.kl_coef,
                            g.entropy_coef, g.scale, (float)(1.0 - g.clip_low), (float)(1.0 + g.clip_high)};
     const double w_all = 1.0 / ((double)q.B * q.G * q.T);           // every step counts: both means are one
     const bool few = (int64_t)q.B * q.T <= PL_FEW && q.B <= PL_INPUTS;
     if (q.eff && !few) {
-        hipLaunchKernelGGL(k_policy_count, dim3(q.B < PL_GRID ? q.B : PL_GRID), dim3(PL_BLOCK), 0, st, q.eff, q.B, q.T, n);
-        hipLaunchKernelGGL(k_policy_weights, dim3(1), dim3(PL_BLOCK), 0, st, n, q.B, q.G, g.by_schedule, w);
+        auto grid = [&](int64_t per) { const int64_t c = (q.B + per - 1) / per; return (int)(c < PL_GRID ? c : PL_GRID); };
+        int parts = 0;
+        auto count = [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            parts = grid(PL_BLOCK / L);
+            hipLaunchKernelGGL(k_policy_count<L>, dim3(parts), dim3(PL_BLOCK), 0, st, q.eff, q.B, q.T, g.by_schedule, n, part);
+        };
+        if (q.T >= 512) count(std::integral_constant<int, 256>{});  // (at least two flags per lane)
+        else if (q.T >= 128) count(std::integral_constant<int, 64>{});
+        else if (q.T >= 16) count(std::integral_constant<int, 8>{});
+        else count(std::integral_constant<int, 1>{});
+        hipLaunchKernelGGL(k_policy_weights, dim3(grid(PL_BLOCK)), dim3(PL_BLOCK), 0, st, n, part, parts, q.B, q.G, g.by_schedule, w);
     } else w = nullptr;
     const int rows = q.B * q.G * q.T;
     const int grid = q.dtype == 1 ? (q.ref_logits ? launch_rows<bf16_t, true>(q, pc, w_all, w, partial, rows, st)

@@ -414,6 +414,30 @@ def test_the_largest_number_of_rows(ctx):
     assert ctx.device_status() == sol.OK
 
 
+@pytest.mark.parametrize("mean", ["steps", "schedules"])
+@pytest.mark.parametrize("B,T", [(300, 1), (5000, 1), (600001, 3), (257, 15), (300, 16), (70000, 17), (300, 130), (9000, 129), (9, 513), (8, 2048), (2, 4096),
+                                 (1, 100003), (3000, 600)])
+def test_many_flags(ctx, B, T, mean):
+    """Shares of the steps where a kernel of their own counts them: policy terms are the advantages themselves (rho = 1), small integers, so
+    that the loss is off by the sum's roundings in 64 bits (2^-53 of the terms' magnitudes each) and one to 32 bits."""
+    gen = torch.Generator(device="cuda").manual_seed(B + T)
+    eff = (torch.rand(B, T, generator=gen, device="cuda") < 0.6).int()
+    eff[torch.rand(B, generator=gen, device="cuda") < 0.2] = 0
+    eff[B // 2, T // 2] = 7
+    adv = torch.randint(-8, 9, (B, 2, T), generator=gen, device="cuda").float()
+    ids = torch.randint(0, 2, (B, 2, T), generator=gen, device="cuda", dtype=torch.int32)
+    got = ctx.policy_loss(torch.zeros(B, 2, T, 2, device="cuda"), ids, adv, eff=eff, mean=mean)
+    on, a = host(eff) != 0, host(adv).astype(np.float64)
+    n = on.sum(1, keepdims=True).astype(np.float64)
+    w = on / (2.0 * n.sum()) if mean == "steps" else on / np.maximum(n, 1.0) / (2.0 * (n > 0).sum())
+    want = -(a * w[:, None]).sum()
+    assert abs(float(got["loss"]) - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -53 * 8 * 2000
+    assert np.array_equal(host(got["logp"]) == 0.0, np.broadcast_to(~on[:, None], a.shape))
+    grad = host(got["grad"]).astype(np.float64)
+    sign = 2.0 * host(ids) - 1.0
+    np.testing.assert_allclose(grad[..., 1], -0.5 * sign * a * w[:, None], rtol=16 * 2.0 ** -24, atol=0)      # w A (p - 1), a few roundings
+
+
 def test_log_probabilities_do_not_go_into_an_input(ctx):
     x, ids, kw = _case(1, 2, 3, 8, seed=23)
     buf, cfg = torch.zeros(32, device="cuda"), sol.PolicyCfg(0.2, 0.2, 0.0, 0.0, 1.0, 1.0, 0)
