@@ -298,8 +298,8 @@ int sol_reward_advantages(sol_ctx *ctx, const float *nll, const int32_t *action_
  * logits is refused, and elements between the rows are left as they are. Where the reference forbids an action that the policy allows,
  * KL is infinite, and with kl_coef > 0 the row's gradient is not finite. A row's elements are summed in 32 bits, its log-probability,
  * the test of the ratio's bounds and the sums over the rows are in 64; a gradient is rounded once. The order of a row's sums depends
- * on A, on the number of elements that the row begins behind a 16-byte boundary and on nothing else. Workspace:
- * sol_policy_workspace_bytes(B, G, T), device memory of any alignment.
+ * on A, on the number of elements that the row begins behind a 16-byte boundary and on whether all rows begin at such boundaries, not
+ * on the other rows' number or values. Workspace: sol_policy_workspace_bytes(B, G, T), device memory of any alignment.
  * B * G * T == 0 is a no-op (loss_out is left as it is); at most 2^31 - 1 rows of 2^30 actions. */
 #define SOL_MEAN_STEPS 0
 #define SOL_MEAN_SCHEDULES 1

@@ -394,11 +394,13 @@ def policy_loss(logits, action_ids, adv=None, old_logp=None, ref_logp=None, ref_
         free, held = ratio * advantage, np.clip(ratio, 1 - clip[0], 1 + clip[1]) * advantage
         clipped = held < free
         by_logp, kl, far = 0.0 if clipped else -free, 0.0, np.zeros(A)
+        by_size = abs(by_logp)
         entropy = -(p * lp0).sum()
         if ref_logp is not None:
             u = float(ref_logp[b, g, t]) - logp
             kl = np.expm1(u) - u
-            by_logp -= kl_coef * np.expm1(u)
+            by_logp -= kl_coef * np.expm1(u)                                 # (may cancel the policy term: its own terms, not the difference)
+            by_size += kl_coef * (np.exp(u) + abs(u) + 1.0)
         if ref_logits is not None:
             far = np.where(some, lp0 - np.where(some, _log_softmax(ref_logits[b, g, t], temperature), 0.0), 0.0)
             kl = (p * far).sum()
@@ -407,7 +409,7 @@ def policy_loss(logits, action_ids, adv=None, old_logp=None, ref_logp=None, ref_
         f = w * scale / temperature
         exact = 0.0 if ref_logits is None else kl_coef
         out["grad"][b, g, t] = f * (by_logp * (hot - p) + exact * p * (far - kl) + entropy_coef * p * (lp0 + entropy))
-        out["size"][b, g, t] = f * (abs(by_logp) * (hot + p) + exact * p * (abs(far) + abs(kl)) + entropy_coef * p * (abs(lp0) + entropy))
+        out["size"][b, g, t] = f * (by_size * (hot + p) + exact * p * (abs(far) + abs(kl)) + entropy_coef * p * (abs(lp0) + entropy))
         out["logp"][b, g, t], out["ratio"][b, g, t] = logp, ratio
         stats += w * np.array([-min(free, held), kl, entropy, float(clipped)])
     out["stats"] = stats

@@ -454,15 +454,15 @@ __device__ __forceinline__ double lanes_sum_f64(double v)
 }
 
 // A row in the registers of LANES lanes, CH pieces of 16 bytes per lane: it is read once, all lanes wait for nothing but the row's
-// maximum and its sums. LANES <= 64: several rows per wave, side by side, no LDS. Bound by memory from rows of about 500 logits on
+// maximum and its sums. LANES < 64: several rows per wave, side by side, no LDS. Bound by memory from rows of about 500 logits on
 // (16288 rows of 4001 fp32 logits with a reference, a fifth of them not effective: 147 us, 4.6 TB/s), below by the row's scalars (512 rows of
-// 64: 4.4 us, 32768: 7.9), where lanes that share a row all compute them.
+// 64: 5.2 us, 32768: 7.1), where lanes that share a row all compute them.
 template <class T, bool EXACT, int LANES, int CH>
-__global__ void __launch_bounds__(LANES > PL_BLOCK ? LANES : PL_BLOCK, LANES == 512 ? 4 : 1)
+__global__ void __launch_bounds__(LANES > 64 ? LANES : PL_BLOCK, LANES == 512 ? 4 : 1)
 k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__restrict__ w_in, double *__restrict__ partial)
 {
     using P = PolicyPiece<T, EXACT, false>;
-    constexpr int V = P::V, BLOCK = LANES > PL_BLOCK ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
+    constexpr int V = P::V, BLOCK = LANES > 64 ? LANES : PL_BLOCK, ROWS = BLOCK / LANES;
     __shared__ float s_max[2][16], s_sum[5][16];
     __shared__ double s_part[ROWS][4];                              // a group's share of the means, its first lane's alone
     __shared__ PolicyShares few;
@@ -543,11 +543,13 @@ k_policy_held(PolicyArgs q, PolicyScalars pc, double w_all, const double *__rest
         }
     }
     __syncthreads();
-    if (tid < 4) {
+    if (tid < 64) {                                                 // sixteen lanes per sum, in a fixed order
         double v = 0.0;
-#pragma unroll 4
-        for (int i = 0; i < ROWS; ++i) v += s_part[i][tid];
-        partial[4 * (int64_t)blockIdx.x + tid] = v;
+#pragma unroll
+        for (int i = 0; i < (ROWS + 15) / 16; ++i) if (const int g = 16 * i + (tid >> 2); g < ROWS) v += s_part[g][tid & 3];
+#pragma unroll
+        for (int o = 4; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+        if (tid < 4) partial[4 * (int64_t)blockIdx.x + tid] = v;
     }
 }
 
@@ -756,7 +758,7 @@ k_policy_stream(PolicyArgs q, PolicyScalars pc, double w_all, const double *__re
         for (int i = 0; i < 4; ++i) partial[4 * (int64_t)blockIdx.x + i] = sum[i];
 }
 
-// The workgroups' sums in a fixed order; stats: policy term, KL, entropy, clipped share. Latency: 2.1 us for a minibatch's 16 partial sums,
+// The workgroups' sums in a fixed order; stats: policy term, KL, entropy, clipped share. Latency: 2.2 us for a minibatch's 8 partial sums,
 // 4.0 for 2048 (1024 threads: 3.6 and 4.0).
 constexpr int PL_FINISH = 256;
 __global__ void __launch_bounds__(PL_FINISH)
@@ -789,10 +791,13 @@ k_policy_finish(const double *__restrict__ partial, int n, PolicyScalars pc, flo
 }
 
 // The row's kernel by its number of 16-byte pieces. Rows of up to 64 KB (32 of bf16 with a reference) stay in the registers of as few lanes as
-// hold them, so that many rows are under way per CU and few lanes repeat a row's scalars; longer ones fill the registers of a CU by
+// hold them at up to 8 pieces each (6 or less leave room for another wave), so that many rows are under way per CU and few lanes repeat a
+// row's scalars; the number of rows has no say, so that a row's result does not depend on it. Longer ones fill the registers of a CU by
 // one or two, and load ahead (k_policy_ring); what does not fit is read twice. Measured, 200 M logits (bytes read and written / time, of
 // 5.06 TB/s that a copy of 1 GiB reaches):
-//   4096 bf16 logits: 64 lanes x 8 pieces 4.8 TB/s, 256 x 4 (two pieces each, two barriers per row) 3.6
+//   8 bf16 logits: a lane per row 2.5 TB/s, 8 lanes 0.4;  64: 4 lanes x 2 pieces 3.8, 8 x 1 2.7;  320: 8 x 6 4.5, 16 x 4 3.8;  4200: 128 x 6
+//   4.0, 256 x 4 3.3;  32 fp32: 4 x 2 4.0, 8 x 1 2.9, 2 x 4 3.6 (64 fp32, 4 x 4 against 8 x 2: 512 rows, all latency, 5.2 us and 4.4, 3.1 M rows 333 and 374)
+//   4096 bf16 logits: 64 lanes x 8 pieces 4.8, 256 x 4 (two pieces each, two barriers per row) 3.6
 //   32768 bf16: 512 x 8 4.7, two sweeps 3.7;  65536 bf16: ring of 512 4.7, one workgroup of 1024 without loading ahead 3.8, two sweeps 3.7
 //   128256 bf16: ring of 1024 4.0 (4.4 where rows fill the CUs evenly), not loading ahead 3.2, two sweeps 3.6
 //   32000 fp32: ring 5.1, two sweeps 4.2;  32000 fp32 with a reference: ring 4.8, two sweeps 3.3
@@ -810,7 +815,7 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
         hipLaunchKernelGGL(kern, dim3(grid), dim3(block), 0, st, q, pc, w_all, w, partial);
     };
     auto held = [&](auto lanes, auto ch) {
-        constexpr int L = decltype(lanes)::value, C = decltype(ch)::value, BLOCK = L > PL_BLOCK ? L : PL_BLOCK;
+        constexpr int L = decltype(lanes)::value, C = decltype(ch)::value, BLOCK = L > 64 ? L : PL_BLOCK;
         go(k_policy_held<T, EXACT, L, C>, BLOCK, BLOCK / L);
     };
     auto ring = [&](auto block, auto ch) {                          // as many workgroups as fit the chip: 16 waves per CU
@@ -820,13 +825,20 @@ static int launch_rows(const PolicyArgs &q, const PolicyScalars &pc, double w_al
         hipLaunchKernelGGL((k_policy_ring<T, EXACT, BLOCK, decltype(ch)::value>), dim3(grid), dim3(BLOCK), 0, st, q, pc, w_all, w, partial);
     };
 #define N(n) std::integral_constant<int, n>{}
-    if (pieces <= 8) held(N(8), N(1));
-    else if (pieces <= 16) held(N(8), N(2));
+    if (pieces <= 1) held(N(1), N(1));
+    else if (pieces <= 2) held(N(1), N(2));
+    else if (pieces <= 4) held(N(2), N(2));
+    else if (pieces <= 8) held(N(4), N(2));
+    else if (pieces <= 16) held(N(4), N(4));
     else if (pieces <= 32) held(N(8), N(4));
-    else if (pieces <= 64) held(N(16), N(4));
-    else if (pieces <= 128) held(N(32), N(4));
-    else if (pieces <= 256) held(N(64), N(4));
+    else if (pieces <= 48) held(N(8), N(6));
+    else if (pieces <= 64) held(N(8), N(8));
+    else if (pieces <= 96) held(N(16), N(6));
+    else if (pieces <= 128) held(N(16), N(8));
+    else if (pieces <= 192) held(N(32), N(6));
+    else if (pieces <= 256) held(N(32), N(8));
     else if (pieces <= 512) held(N(64), N(8));
+    else if (!EXACT && pieces <= 768) { if constexpr (!EXACT) held(N(128), N(6)); }
     else if (pieces <= 1024) held(N(256), N(4));
     else if (pieces <= 2048) held(N(256), N(8));
     else if constexpr (HEAVY) go(k_policy_stream<T, EXACT, 512, 2>, 512, 1);

@@ -4,7 +4,8 @@ Tolerances, derived: with t_j = (x_j - m) log2(e) / temperature, e_j = 2^t_j car
 ln2 * 3 * 2^-24 |t_j| relative, plus one step of 2^x; a sum of A terms at most min(A, 600) additions in one lane (and 16 across lanes)
 plus the errors of its terms; a coefficient at most 16 further roundings. A gradient is a sum of products of these, so its error is at
 most R * 2^-24 times the sum of the magnitudes it is made of (the oracle's `size`), R = 2 * 2.1 * max|t| + min(A, 600) + 48, plus half a
-step of its type. Elements whose |t| is over 60 have p < 2^-60 and are held to that share of their row.
+step of its type. The magnitudes are those before any difference is taken: where the policy term -rho A and the KL term c (1 - e^u) cancel to
+G, G is off by the roundings of both, 2^-24 (|rho A| + c (e^u + |u| + 1)), which no multiple of |G| bounds. Elements whose |t| is over 60 have p < 2^-60 and are held to that share of their row.
 The term m log2(e) / temperature in t is itself rounded: every t of a row is off by the same amount, at most 2^-24 |m| log2(e) / temperature =
 2^-24 M. It cancels in p, H and KL, but not in the roundings of the sums and products that hold it: at most 16 of 2^-23 each, so that
 2^-43 M (times weights and coefficients below 1) remains also where all true terms are 0, as for a single action. Rows with M > 2^22 are
@@ -115,6 +116,18 @@ def test_every_length_against_the_oracle(ctx, A, dtype, kl):
 @pytest.mark.parametrize("kl", ["none", "logp", "logits"])
 def test_padded_and_unaligned_rows(ctx, A, pad, offset, dtype, kl):
     x, ids, kw = _case(1, 2, 3, A, dtype, pad, offset, kl, forbid=7 if A > 7 else 0, temperature=1.3, seed=2)
+    got = _run(ctx, x, ids, kw)
+    assert ctx.device_status() == sol.OK
+    _check(got, _oracle(x, ids, kw), x, kw, _rel(x, kw))
+
+
+@pytest.mark.parametrize("A", [4, 8, 12, 16, 24, 31, 32, 48, 63, 96, 127, 128, 160, 191, 192, 200, 255, 256, 320, 383, 384, 511, 512, 640, 767, 768, 769, 1023,
+                               1025, 1535, 1537, 2047, 2049, 2500, 4097, 6143, 6145])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kl", ["logp", "logits"])
+def test_lengths_that_lanes_share_in_another_way(ctx, A, dtype, kl):
+    """Rows on both sides of the lengths at which more lanes take a row, more of them than one workgroup holds, some not effective."""
+    x, ids, kw = _case(3, 11, 9, A, dtype, kl=kl, ragged=True, seed=31)
     got = _run(ctx, x, ids, kw)
     assert ctx.device_status() == sol.OK
     _check(got, _oracle(x, ids, kw), x, kw, _rel(x, kw))
