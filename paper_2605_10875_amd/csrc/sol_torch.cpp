@@ -1,6 +1,6 @@
 // What the binding does with torch tensors on the way to include/sol.h, where Python would take longer than the GPU: the lists of the
 // operators over many tensors (0.3 us of attribute calls per tensor, 5 lists of 224: 385 us; here 10 ns), and the arguments and outputs
-// of the policy loss (10 us for a minibatch whose kernels take 8; here 3). Marshalling only; the library's entry points come as addresses.
+// of the clip and of the policy loss (10 us for a minibatch whose kernels take 8; here 3). Marshalling only; the library's entry points come as addresses.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -128,7 +128,64 @@ PyObject *policy_loss_args(PyObject *const *a, Py_ssize_t n)
     return all;
 }
 
+// why an entry of a list is refused, nullptr if it is not. types: the allowed element types (1 float32, 2 bfloat16, 3 either)
+const char *refusal(PyObject *o, long types, int64_t device)
+{
+    if (!THPVariable_Check(o)) return "a tensor is needed";
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const int code = code_of(t);
+    if (code > 1 || !(types >> code & 1)) return types == 1 ? "float32 is needed" : types == 2 ? "bfloat16 is needed" : "float32 or bfloat16 is needed";
+    if (!here(t, device)) return "not on the current device";
+    return t.is_contiguous() ? nullptr : "has to be contiguous";
+}
+
+PyObject *grad_clip_args(PyObject *const *a, Py_ssize_t n)
+{
+    need(n == 9, "grad_clip", "9 arguments are needed");
+    auto whole = [&](int i) { const long long v = PyLong_AsLongLong(a[i]); if (v == -1 && PyErr_Occurred()) throw python_error(); return (int64_t)v; };
+    auto real = [&](int i) { const double v = PyFloat_AsDouble(a[i]); if (v == -1.0 && PyErr_Occurred()) throw python_error(); return v; };
+    const auto clip_fn = (decltype(&sol_grad_clip))whole(0);
+    const auto size_fn = (decltype(&sol_grad_clip_workspace_bytes))whole(1);
+    const int64_t device = whole(3);
+    const double max_norm = real(6), eps = real(7);
+    THPObjectPtr list(PySequence_Fast(a[5], "a list of tensors is needed"));
+    if (!list) throw python_error();
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(list.get());
+    need(count <= INT32_MAX, "grads", "more tensors than 32 bits count");
+    std::vector<sol_grad> grads((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject *const o = PySequence_Fast_GET_ITEM(list.get(), i);
+        if (const char *const why = refusal(o, 3, device)) throw Refused{"grads[" + std::to_string(i) + "]: " + why};
+        const at::Tensor &t = THPVariable_Unpack(o);
+        grads[(size_t)i] = sol_grad{t.data_ptr(), t.numel(), code_of(t), 0};
+    }
+    const size_t bytes = size_fn((int)count);
+    const at::Tensor out = at::empty({2 + (int64_t)bytes / 4 + 1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (at::DeviceIndex)device));
+    float *const at0 = (float *)out.data_ptr();
+    const int rc = clip_fn((sol_ctx *)whole(2), grads.data(), (int)count, max_norm, eps, whole(8) != 0, at0, at0 + 1, at0 + 2, bytes, (void *)whole(4));
+    if (rc) return PyLong_FromLong(rc);
+    PyObject *const all = PyTuple_New(3);
+    PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(out.narrow(0, 0, 1)));
+    PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(out.narrow(0, 1, 1)));
+    PyTuple_SET_ITEM(all, 2, THPVariable_Wrap(out));
+    return all;
+}
+
 }  // namespace
+
+// grad_clip(entry point, workspace size function, context, device, stream, grads, max_norm, eps, scale) -> a status, or (norm, coef, the
+// buffer that holds both and the workspace)
+static PyObject *py_grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    try {
+        return grad_clip_args(a, n);
+    } catch (const Refused &r) {
+        PyErr_SetString(PyExc_ValueError, r.what.c_str());
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
 
 // policy_loss(entry point, workspace size function, context, device, stream, logits, action_ids, adv, old_logp, ref_logp, ref_logits, eff,
 // want_grad, grad_out, clip_low, clip_high, kl_coef, entropy_coef, temperature, scale, mean) -> a status, or (loss, stats, logp,
@@ -174,21 +231,14 @@ static PyObject *tensor_lists_args(PyObject *const *a, Py_ssize_t n)
         const long types = PyLong_AsLong(PyTuple_GET_ITEM(a[2], k));
         for (Py_ssize_t i = 0; i < count; ++i) {
             int64_t *const w = words + i * (K + 2);
-            const char *why = nullptr;
             PyObject *const o = PySequence_Fast_GET_ITEM(lists[k].get(), i);
-            if (!THPVariable_Check(o)) why = "a tensor is needed";
-            else {
+            const char *why = refusal(o, types, device);
+            if (!why) {
                 const at::Tensor &t = THPVariable_Unpack(o);
-                const int code = code_of(t);
-                if (code > 1 || !(types >> code & 1)) why = types == 1 ? "float32 is needed" : types == 2 ? "bfloat16 is needed" : "float32 or bfloat16 is needed";
-                else if (!here(t, device)) why = "not on the current device";
-                else if (!t.is_contiguous()) why = "has to be contiguous";
-                else if (k > 0 && lists[0] && w[K] != t.numel()) why = "not as many elements as the tensor of the first list";
-                else {
-                    w[k] = (int64_t)(uintptr_t)t.data_ptr();
-                    w[K] = t.numel();
-                    if (k == typed) w[K + 1] = code;
-                }
+                if (k > 0 && lists[0] && w[K] != t.numel()) why = "not as many elements as the tensor of the first list";
+                w[k] = (int64_t)(uintptr_t)t.data_ptr();
+                w[K] = t.numel();
+                if (k == typed) w[K + 1] = code_of(t);
             }
             if (why) throw Refused{std::string(PyUnicode_AsUTF8(PyTuple_GET_ITEM(a[1], k))) + "[" + std::to_string(i) + "]: " + why};
         }
@@ -209,6 +259,7 @@ static PyObject *py_tensor_lists(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 static PyMethodDef methods[] = {
     {"policy_loss", (PyCFunction)(void (*)(void))py_policy_loss, METH_FASTCALL, nullptr},
+    {"grad_clip", (PyCFunction)(void (*)(void))py_grad_clip, METH_FASTCALL, nullptr},
     {"tensor_lists", (PyCFunction)(void (*)(void))py_tensor_lists, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 static PyModuleDef module = {PyModuleDef_HEAD_INIT, "sol_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -280,7 +280,7 @@ class Sol:
         if rc:
             raise SolError(rc, (self.L.sol_last_error(None) or b"").decode())
         self._ws = None
-        self._policy = None
+        self._policy = self._clip = None
 
     def close(self):
         if self.handle:
@@ -509,16 +509,15 @@ class Sol:
     def grad_clip(self, grads, max_norm, eps=1e-6, scale=True, stream=None):
         """Norm over all gradients (contiguous float32 or bfloat16 tensors) and coef = min(1, max_norm / (norm + eps)), both float32
         [1] on the device; scale: the gradients are multiplied by coef in place. Nothing is synchronised."""
-        words = _native().tensor_lists((grads,), ("grads",), (3,), 0, torch.cuda.current_device())
-        n = len(grads)
-        out = torch.empty(2, dtype=torch.float32, device="cuda")
-        need = self.L.sol_grad_clip_workspace_bytes(n)
-        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-        at = out.data_ptr()
-        self._check(self.L.sol_grad_clip(self.handle, words, n, max_norm, eps, int(bool(scale)), at, at + 4, ws.data_ptr(), need,
-                                         _stream(stream)))
-        _used_on(stream, ws, out)
-        return out[:1], out[1:]
+        if self._clip is None:
+            self._clip = (_native().grad_clip, _address(self.L.sol_grad_clip), _address(self.L.sol_grad_clip_workspace_bytes))
+        call, entry, sizes = self._clip
+        got = call(entry, sizes, self.handle.value or 0, torch.cuda.current_device(), _stream(stream).value or 0, grads, max_norm, eps, bool(scale))
+        if type(got) is int:
+            self._check(got)
+        norm, coef, out = got
+        _used_on(stream, out)
+        return norm, coef
 
     def adamw_step(self, params, grads, exp_avg, exp_avg_sq, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, coef=None,
                    copies=None, stream=None):

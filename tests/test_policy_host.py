@@ -139,3 +139,18 @@ def test_the_binding_is_compiled_with_the_library(tmp_path, monkeypatch):
     before = (tmp_path / "part.so").stat().st_mtime_ns
     build.build_torch(force=False)
     assert (tmp_path / "part.so").stat().st_mtime_ns == before
+
+
+@pytest.mark.parametrize("grads,word", [([3], r"grads\[0\]: a tensor"), ([torch.zeros(2), torch.zeros(2).double()], r"grads\[1\]: float32 or bfloat16"),
+                                        ([torch.zeros(4, 2).t()], r"grads\[0\]: has to be contiguous"), ([torch.zeros(2).to_sparse()], r"grads\[0\]: not on the current"),
+                                        ([None], r"grads\[0\]: a tensor"), ((torch.zeros(2, device="meta"),), r"grads\[0\]: not on the current")])
+def test_grad_clip_refuses(ctx, monkeypatch, grads, word):
+    ctx._clip = None
+    if grads[0] is not None and getattr(grads[0], "is_meta", False):
+        monkeypatch.setattr(sol.torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match=word):
+        ctx.grad_clip(grads, 1.0)
+    with pytest.raises(TypeError):
+        ctx.grad_clip(5, 1.0)
+    with pytest.raises(TypeError):
+        ctx.grad_clip([], "1")
